@@ -244,6 +244,69 @@ int gspn_proxy_project_bwd_static(const void* gout, const void* in, const void* 
 /* "mfma" or "fma": which kernel gspn_proxy_project runs for these arguments ("invalid" for bad ones). */
 const char* gspn_proxy_plan(int B, int K, int M, int H, int W, int dtype);
 
+/* The operators around the scan in a block that uses it: a projection with what follows it, the gated feed-forward pair and cross attention,
+ * all on [B][channels][H][W] maps as the scan has them.  Pointers, element types, stream and errors as for the scan calls; bias and gradients
+ * of matrices and biases are stored in the storage type like the matrices themselves; products and sums are fp32, each stored value is
+ * rounded once.  An activation code that is none of these is GSPN_ERR_UNSUPPORTED. */
+enum { GSPN_ACT_NONE = 0, GSPN_ACT_SILU = 1, GSPN_ACT_GELU = 2, GSPN_ACT_SIGMOID = 3 };   /* z; z/(1+exp(-z)); z*(1+erf(z/sqrt 2))/2; 1/(1+exp(-z)) */
+
+/* gspn_proxy_project with bias, activation and residual in the same launch (the scan's parameters from a map: lambda and u by a sigmoid, logits
+ * with a bias; the way back up with the block's residual):
+ *     out[b][m][n] = act(sum_k P[m][k] in[b][k][n] + bias[m]) + residual[b][m][n]          n = pixel
+ *   in [B,K,H,W]; P [M,K]; bias [M] or NULL; residual [B,M,H,W] or NULL; out [B,M,H,W]
+ * A matrix of 2^31 or more values, and maps whose tiles no launch counts, are GSPN_ERR_UNSUPPORTED. */
+int gspn_proxy_project_fused(const void* in, const void* P, const void* bias, const void* residual, void* out,
+                             int B, int K, int M, int H, int W, int act, int dtype, void* stream);
+/* Its gradients, given gout = dL/dout.  Nothing is kept from the forward call: with an activation the product is computed again.
+ *     g = gout * act'(P in + bias);  gin = P^T g;  gP = sum over b, n of g in^T;  gbias = sum over b, n of g;  the residual's gradient is gout
+ *   gin [B,K,H,W], gP [M,K], gbias [M]: out, in the storage type, or NULL (not computed; one of them at least).  With an activation and 16-bit storage g is
+ *   rounded to the storage type for the products of gin and gP (gbias adds it unrounded).
+ *   workspace: device memory of the caller's, 16-byte aligned, of at least gspn_proxy_project_fused_bwd_bytes bytes (fewer: GSPN_ERR_SHAPE), overwritten by
+ *   the call, free again when its work on `stream` is done; calls that may overlap need one each.  No atomics: the result is bitwise
+ *   repeatable. */
+int gspn_proxy_project_fused_bwd(const void* gout, const void* in, const void* P, const void* bias, void* gin, void* gP, void* gbias,
+                                 void* workspace, unsigned long long workspace_bytes,
+                                 int B, int K, int M, int H, int W, int act, int dtype, void* stream);
+/* 0 for arguments that the call refuses. */
+unsigned long long gspn_proxy_project_fused_bwd_bytes(int B, int K, int M, int H, int W, int act, int dtype);
+
+/* The gated feed-forward pair: both projections, the activation and the product in one launch.  P holds the rows of the gate, then those of the
+ * other projection:
+ *     out[b][f][n] = act(sum_k P[f][k] in[b][k][n] + bias[f]) * (sum_k P[F+f][k] in[b][k][n] + bias[F+f])
+ *   in [B,K,H,W]; P [2F,K]; bias [2F] or NULL; out [B,F,H,W].  (The way back down is gspn_proxy_project_fused.) */
+int gspn_gated_project(const void* in, const void* P, const void* bias, void* out,
+                       int B, int K, int F, int H, int W, int act, int dtype, void* stream);
+/* Its gradients: gin [B,K,H,W], gP [2F,K], gbias [2F]; rounding, workspace (gspn_gated_project_bwd_bytes) and repeatability as above. */
+int gspn_gated_project_bwd(const void* gout, const void* in, const void* P, const void* bias, void* gin, void* gP, void* gbias,
+                           void* workspace, unsigned long long workspace_bytes,
+                           int B, int K, int F, int H, int W, int act, int dtype, void* stream);
+unsigned long long gspn_gated_project_bwd_bytes(int B, int K, int F, int H, int W, int act, int dtype);
+
+/* Cross attention of a map's positions to the states of an encoder (the attention that a scan does not stand in for):
+ *     s[t] = scale * sum_d k[b][t][h'][d] q[b][h][d][n] ;  p = softmax of s over the tokens that take part ;  out[b][h][d][n] = sum_t p[t] v[b][t][h'][d]
+ *   q, out [B,heads*D,H,W]; k, v [B,L,kv_heads*D], head h of the map with head h' = h / (heads/kv_heads) of the tokens
+ *   mask   [B,L] bytes, 0: the token takes no part (whatever k and v hold for it is never used); NULL: all take part
+ *   lse    [B,heads,H,W] fp32, log of the sum of exp(s), for the backward call; or NULL
+ * A position whose image has no token that takes part gets out = 0 and lse = -inf.  heads must be a multiple of kv_heads, scale positive and finite (else
+ * GSPN_ERR_SHAPE); D a multiple of 8 and at most GSPN_MAX_HEAD, L at most GSPN_MAX_TOKENS (else GSPN_ERR_UNSUPPORTED).  The weights p are
+ * rounded to the storage type for the product with v; the sums of both are fp32.
+ *   workspace: calls of few positions and many tokens cut the tokens into stretches, given gspn_cross_attention_bytes bytes (0: no use for any) of device
+ *   memory under the terms above; NULL: the same result up to rounding, without the stretches. */
+enum { GSPN_MAX_HEAD = 128, GSPN_MAX_TOKENS = 1 << 24 };
+int gspn_cross_attention(const void* q, const void* k, const void* v, const unsigned char* mask, void* out, float* lse,
+                         void* workspace, unsigned long long workspace_bytes,
+                         int B, int heads, int kv_heads, int D, int H, int W, int L, float scale, int dtype, void* stream);
+unsigned long long gspn_cross_attention_bytes(int B, int heads, int kv_heads, int D, int H, int W, int L, int dtype);
+/* Its gradients, given gout = dL/dout, and out and lse of the forward call with the same arguments:
+ *     ds = p * (sum_d v gout - sum_d gout out);  gq = scale sum_t ds k;  gk = scale sum ds q;  gv = sum p gout   (gk, gv over the positions of all heads
+ *     that share the token's head; 0 for tokens that take no part)
+ *   gq [B,heads*D,H,W], gk, gv [B,L,kv_heads*D]: out, or NULL (not computed; one of them at least); workspace (required) of
+ *   gspn_cross_attention_bwd_bytes bytes under the terms above.  p and ds are rounded to the storage type for the products.  No atomics. */
+int gspn_cross_attention_bwd(const void* gout, const void* q, const void* k, const void* v, const unsigned char* mask, const void* out, const float* lse,
+                             void* gq, void* gk, void* gv, void* workspace, unsigned long long workspace_bytes,
+                             int B, int heads, int kv_heads, int D, int H, int W, int L, float scale, int dtype, void* stream);
+unsigned long long gspn_cross_attention_bwd_bytes(int B, int heads, int kv_heads, int D, int H, int W, int L, int dtype);
+
 /* Name of the kernel family the forward / backward call would dispatch to for
  * these arguments: "plane" (small maps, whole planes through LDS), "pair" (128x128 maps in 16-bit storage
  * with an even number of channels per weight group, all four directions, the global scan or GSPN-local, normalised

@@ -21,6 +21,7 @@ from typing import Optional
 GSPN_F32, GSPN_BF16, GSPN_F16 = 0, 1, 2
 GSPN_FLAG_SHARED_PARAMS = 1
 DIR_ALL = 15
+GSPN_ACT_NONE, GSPN_ACT_SILU, GSPN_ACT_GELU, GSPN_ACT_SIGMOID = 0, 1, 2, 3
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -30,6 +31,9 @@ EXPORTS = ("gspn_scan_fwd", "gspn_scan_bwd", "gspn_scan_fwd_local", "gspn_scan_b
            "gspn_fwd_plan", "gspn_bwd_plan", "gspn_fwd_local_plan", "gspn_bwd_local_plan",
            "gspn_fwd_logits_plan", "gspn_bwd_logits_plan", "gspn_proxy_project", "gspn_proxy_project_bwd", "gspn_proxy_project_bwd_static", "gspn_proxy_plan",
            "gspn_scan_fwd_transposed", "gspn_fwd_transposed_plan", "gspn_scan_fwd_unfused", "gspn_unfused_workspace_bytes",
+           "gspn_proxy_project_fused", "gspn_proxy_project_fused_bwd", "gspn_proxy_project_fused_bwd_bytes",
+           "gspn_gated_project", "gspn_gated_project_bwd", "gspn_gated_project_bwd_bytes",
+           "gspn_cross_attention", "gspn_cross_attention_bytes", "gspn_cross_attention_bwd", "gspn_cross_attention_bwd_bytes",
            "gspn_status_string", "gspn_version", "gspn_reload_env")
 
 
@@ -102,6 +106,18 @@ def load_library() -> ctypes.CDLL:
     lib.gspn_fwd_plan.restype = ctypes.c_char_p
     lib.gspn_bwd_plan.argtypes = [ci] * 5 + [cu, ci, cu]
     lib.gspn_bwd_plan.restype = ctypes.c_char_p
+    ull, cf = ctypes.c_ulonglong, ctypes.c_float
+    lib.gspn_proxy_project_fused.argtypes = [vp] * 5 + [ci] * 7 + [vp]
+    lib.gspn_gated_project.argtypes = [vp] * 4 + [ci] * 7 + [vp]
+    for bwd, size in ((lib.gspn_proxy_project_fused_bwd, lib.gspn_proxy_project_fused_bwd_bytes), (lib.gspn_gated_project_bwd, lib.gspn_gated_project_bwd_bytes)):
+        bwd.argtypes = [vp] * 8 + [ull] + [ci] * 7 + [vp]
+        size.argtypes = [ci] * 7
+        size.restype = ull
+    lib.gspn_cross_attention.argtypes = [vp] * 7 + [ull] + [ci] * 7 + [cf, ci, vp]
+    lib.gspn_cross_attention_bwd.argtypes = [vp] * 11 + [ull] + [ci] * 7 + [cf, ci, vp]
+    for size in (lib.gspn_cross_attention_bytes, lib.gspn_cross_attention_bwd_bytes):
+        size.argtypes = [ci] * 8
+        size.restype = ull
     lib.gspn_status_string.argtypes = [ci]
     lib.gspn_status_string.restype = ctypes.c_char_p
     lib.gspn_version.argtypes = []
@@ -483,3 +499,145 @@ def gspn_scan_fwd_unfused(x, w, lam, u, y, h_save, workspace, *, G: Optional[int
     nbytes = workspace.numel() * workspace.element_size()
     _check(load_library().gspn_scan_fwd_unfused(*ptrs, workspace.data_ptr(), nbytes, B, C, H, W, G, dir_mask,
                                                 _dtype_code(x), flags, _stream(stream)))
+
+
+# ---------------------------------------------------------------- the operators around the scan
+def _need(x, nbytes, workspace, stream, name):
+    """(address, bytes) of a call's workspace: the caller's, or `nbytes` from torch's allocator, which `keep` holds while the call is enqueued."""
+    if workspace is not None:
+        if not workspace.is_cuda or workspace.device != x.device or not workspace.is_contiguous():
+            raise ValueError("workspace: must be a contiguous tensor on the device of the call's tensors")
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+    keep = _workspace(x, nbytes, stream) if nbytes else None
+    if keep is None and name is not None:
+        raise RuntimeError(f"{name}: no memory of torch's allocator for a workspace of {nbytes} bytes on this stream: pass one")
+    return (None, 0, None) if keep is None else (keep.data_ptr(), nbytes, keep)
+
+
+def _maps(t, name):
+    if t.dim() != 4:
+        raise ValueError(f"{name}: must have four dimensions, got shape {tuple(t.shape)}")
+    return t.shape
+
+
+def _product_fwd(f, per, inp, P, out, bias, residual, act, stream):
+    B, K, H, W = _maps(inp, "inp")
+    rows = P.shape[0] if P.dim() == 2 else 0
+    if rows < 1 or rows % per:
+        raise ValueError(f"P: shape {tuple(P.shape)} is not [{'2F' if per == 2 else 'M'}, K]")
+    M = rows // per
+    args = [_ptr(inp, "inp", (B, K, H, W), inp), _ptr(P, "P", (rows, K), inp), _ptr(bias, "bias", (rows,), inp)]
+    if per == 1:
+        args.append(_ptr(residual, "residual", (B, M, H, W), inp))
+    args.append(_ptr(out, "out", (B, M, H, W), inp))
+    _check(f(*args, B, K, M, H, W, act, _dtype_code(inp), _stream(stream)))
+
+
+def _product_bwd(f, size, name, per, gout, inp, P, gin, gP, gbias, bias, act, workspace, stream):
+    B, K, H, W = _maps(inp, "inp")
+    rows = P.shape[0] if P.dim() == 2 else 0
+    if rows < 1 or rows % per:
+        raise ValueError(f"P: shape {tuple(P.shape)} is not [{'2F' if per == 2 else 'M'}, K]")
+    M = rows // per
+    args = [_ptr(gout, "gout", (B, M, H, W), inp), _ptr(inp, "inp", (B, K, H, W), inp), _ptr(P, "P", (rows, K), inp), _ptr(bias, "bias", (rows,), inp),
+            _ptr(gin, "gin", (B, K, H, W), inp), _ptr(gP, "gP", (rows, K), inp), _ptr(gbias, "gbias", (rows,), inp)]
+    dims, code = (B, K, M, H, W), _dtype_code(inp)
+    at, nbytes, keep = _need(inp, size(*dims, act, code), workspace, stream, name)
+    _check(f(*args, at, nbytes, *dims, act, code, _stream(stream)))
+
+
+def gspn_proxy_project_fused(inp, P, out, *, bias=None, residual=None, act: int = GSPN_ACT_NONE, stream=None) -> None:
+    """out = act(P inp + bias) + residual per pixel (see include/gspn.h), in one launch.
+    inp [B,K,H,W]; P [M,K]; bias [M] or None; residual and out [B,M,H,W]; act: GSPN_ACT_*.  Device tensors of one dtype, contiguous."""
+    _product_fwd(load_library().gspn_proxy_project_fused, 1, inp, P, out, bias, residual, act, stream)
+
+
+def gspn_proxy_project_fused_bwd(gout, inp, P, gin, gP, gbias, *, bias=None, act: int = GSPN_ACT_NONE, workspace=None, stream=None) -> None:
+    """Gradients of gspn_proxy_project_fused: gin [B,K,H,W], gP [M,K], gbias [M], all of inp's dtype, each or None; the residual's gradient is gout.
+    bias and act as in the forward call.  workspace: a contiguous device tensor of at least gspn_proxy_project_fused_bwd_bytes bytes, or None:
+    taken from torch's allocator for the call."""
+    lib = load_library()
+    _product_bwd(lib.gspn_proxy_project_fused_bwd, lib.gspn_proxy_project_fused_bwd_bytes, "gspn_proxy_project_fused_bwd", 1,
+                 gout, inp, P, gin, gP, gbias, bias, act, workspace, stream)
+
+
+def gspn_proxy_project_fused_bwd_bytes(B, K, M, H, W, act=GSPN_ACT_NONE, dtype=GSPN_F32) -> int:
+    return int(load_library().gspn_proxy_project_fused_bwd_bytes(B, K, M, H, W, act, dtype))
+
+
+def gspn_gated_project(inp, P, out, *, bias=None, act: int = GSPN_ACT_SILU, stream=None) -> None:
+    """out = act(P[:F] inp + bias[:F]) * (P[F:] inp + bias[F:]) per pixel, in one launch.
+    inp [B,K,H,W]; P [2F,K]; bias [2F] or None; out [B,F,H,W].  Device tensors of one dtype, contiguous."""
+    _product_fwd(load_library().gspn_gated_project, 2, inp, P, out, bias, None, act, stream)
+
+
+def gspn_gated_project_bwd(gout, inp, P, gin, gP, gbias, *, bias=None, act: int = GSPN_ACT_SILU, workspace=None, stream=None) -> None:
+    """Gradients of gspn_gated_project: gin [B,K,H,W], gP [2F,K], gbias [2F], each or None; the rest as gspn_proxy_project_fused_bwd."""
+    lib = load_library()
+    _product_bwd(lib.gspn_gated_project_bwd, lib.gspn_gated_project_bwd_bytes, "gspn_gated_project_bwd", 2,
+                 gout, inp, P, gin, gP, gbias, bias, act, workspace, stream)
+
+
+def gspn_gated_project_bwd_bytes(B, K, F, H, W, act=GSPN_ACT_SILU, dtype=GSPN_F32) -> int:
+    return int(load_library().gspn_gated_project_bwd_bytes(B, K, F, H, W, act, dtype))
+
+
+def _attend_args(q, k, v, mask, heads, kv_heads, scale):
+    B, C, H, W = _maps(q, "q")
+    kv_heads = heads if kv_heads is None else kv_heads
+    if heads < 1 or kv_heads < 1 or heads % kv_heads or C % heads:
+        raise ValueError(f"heads {heads}, kv_heads {kv_heads}: q's {C} channels are heads times a head's, heads a multiple of kv_heads")
+    D = C // heads
+    L = k.shape[1] if k.dim() == 3 else 0
+    args = [_ptr(q, "q", (B, C, H, W), q), _ptr(k, "k", (B, L, kv_heads * D), q), _ptr(v, "v", (B, L, kv_heads * D), q)]
+    if mask is None:
+        args.append(None)
+    else:
+        torch = (_TORCH or _torch())[0]
+        if not mask.is_cuda or mask.device != q.device or mask.dtype not in (torch.bool, torch.uint8) or tuple(mask.shape) != (B, L) or not mask.is_contiguous():
+            raise ValueError(f"mask: must be a contiguous bool or uint8 device tensor of shape {(B, L)}")
+        args.append(mask.data_ptr())
+    return args, (B, heads, kv_heads, D, H, W, L), float(D ** -0.5 if scale is None else scale)
+
+
+def _lse_ptr(lse, q, heads):
+    B, _, H, W = q.shape
+    torch = (_TORCH or _torch())[0]
+    if not lse.is_cuda or lse.device != q.device or lse.dtype != torch.float32 or tuple(lse.shape) != (B, heads, H, W) or not lse.is_contiguous():
+        raise ValueError(f"lse: must be a contiguous float32 device tensor of shape {(B, heads, H, W)}")
+    return lse.data_ptr()
+
+
+def gspn_cross_attention(q, k, v, out, lse=None, *, heads: int, kv_heads: Optional[int] = None, mask=None, scale: Optional[float] = None,
+                         workspace=None, stream=None) -> None:
+    """Attention of the positions of a map to an encoder's tokens (see include/gspn.h).
+    q, out [B,heads*D,H,W]; k, v [B,L,kv_heads*D] (kv_heads None: heads); mask [B,L] bool or uint8 (False: the token takes no part) or None;
+    lse [B,heads,H,W] float32 or None (the backward call needs it); scale None: D ** -0.5.  Device tensors, contiguous.
+    workspace: a device tensor of gspn_cross_attention_bytes bytes, or None: what a call of few positions and many tokens asks for is then taken from torch's
+    allocator, and where there is none it runs without, more slowly and with other roundings."""
+    args, dims, scale = _attend_args(q, k, v, mask, heads, kv_heads, scale)
+    args.append(_ptr(out, "out", q.shape, q))
+    args.append(None if lse is None else _lse_ptr(lse, q, heads))
+    lib, code = load_library(), _dtype_code(q)
+    at, nbytes, keep = _need(q, lib.gspn_cross_attention_bytes(*dims, code), workspace, stream, None)
+    _check(lib.gspn_cross_attention(*args, at, nbytes, *dims, scale, code, _stream(stream)))
+
+
+def gspn_cross_attention_bytes(B, heads, kv_heads, D, H, W, L, dtype=GSPN_F32) -> int:
+    return int(load_library().gspn_cross_attention_bytes(B, heads, kv_heads, D, H, W, L, dtype))
+
+
+def gspn_cross_attention_bwd(gout, q, k, v, out, lse, gq, gk, gv, *, heads: int, kv_heads: Optional[int] = None, mask=None,
+                             scale: Optional[float] = None, workspace=None, stream=None) -> None:
+    """Gradients of gspn_cross_attention, given its out and lse: gq (shape of q), gk and gv (of k), each or None.  workspace: a device tensor of
+    gspn_cross_attention_bwd_bytes bytes, or None: taken from torch's allocator for the call."""
+    args, dims, scale = _attend_args(q, k, v, mask, heads, kv_heads, scale)
+    args = [_ptr(gout, "gout", q.shape, q)] + args + [_ptr(out, "out", q.shape, q), _lse_ptr(lse, q, heads),
+                                                      _ptr(gq, "gq", q.shape, q), _ptr(gk, "gk", k.shape, q), _ptr(gv, "gv", k.shape, q)]
+    lib, code = load_library(), _dtype_code(q)
+    at, nbytes, keep = _need(q, lib.gspn_cross_attention_bwd_bytes(*dims, code), workspace, stream, "gspn_cross_attention_bwd")
+    _check(lib.gspn_cross_attention_bwd(*args, at, nbytes, *dims, scale, code, _stream(stream)))
+
+
+def gspn_cross_attention_bwd_bytes(B, heads, kv_heads, D, H, W, L, dtype=GSPN_F32) -> int:
+    return int(load_library().gspn_cross_attention_bwd_bytes(B, heads, kv_heads, D, H, W, L, dtype))

@@ -1,0 +1,111 @@
+// Host side of the products with an epilogue (gspn_product_impl.hpp): which tile a call runs, and the sums over partial results.
+#include "gspn_product_impl.hpp"
+
+namespace gspn {
+
+namespace {
+
+size_t tiles_of(const ProductParams& p, bool gated, int bm, int bn, int images) {
+    const int rows = gated ? bm / 2 : bm;
+    return (size_t)((p.M + rows - 1) / rows) * ((p.N + bn - 1) / bn) * images;
+}
+
+// Large tiles where they are one for every CU or more; smaller ones, with several waves over the contracted axis, where they are not
+int product_tile(const ProductParams& p, int form, int outcome) {
+    const bool gated = outcome == OUT_GATED || outcome == OUT_GATED_GRAD;
+    if (form == PRODUCT_GRAD_MATRIX) return p.M > 64 && p.N > 64 ? TILE_LARGE : TILE_MEDIUM;
+    if (!gated && p.M <= 32 && tiles_of(p, false, 32, 128, p.images) >= 256) return TILE_FLAT;
+    if (tiles_of(p, gated, 128, 128, p.images) >= 256) return TILE_LARGE;
+    return tiles_of(p, gated, 64, 64, p.images) >= 256 ? TILE_MEDIUM : TILE_SMALL;
+}
+void tile_columns(int tile, int* bn, int* wn) {
+    *bn = tile == TILE_LARGE || tile == TILE_FLAT ? 128 : (tile == TILE_MEDIUM ? 64 : 32);
+    *wn = tile == TILE_FLAT ? 4 : (tile == TILE_SMALL ? 1 : 2);
+}
+
+// 32 neighbouring results per workgroup; eight strips of the parts, added in order
+template <typename T> __global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict__ in, T* __restrict__ out, int parts, size_t n) {
+    __shared__ float strip[8][32];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const size_t i = (size_t)blockIdx.x * 32 + x;
+    float sum = 0.f;
+    if (i < n)
+        for (int k = y; k < parts; k += 8) sum += in[(size_t)k * n + i];
+    strip[y][x] = sum;
+    __syncthreads();
+    if (y == 0 && i < n) {
+#pragma unroll
+        for (int k = 1; k < 8; ++k) sum += strip[k][x];
+        stf(out + i, sum);
+    }
+}
+
+constexpr int ROW_SUM = 4096;                          // values of a row that a wave adds
+template <typename T> __global__ void __launch_bounds__(256) row_sums_kernel(const T* __restrict__ g, float* __restrict__ parts, int images, int M, int N) {
+    const int lane = threadIdx.x & 63, chunks = (N + ROW_SUM - 1) / ROW_SUM;
+    const size_t item = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (item >= (size_t)images * chunks * M) return;
+    const size_t part = item / M;
+    const int m = (int)(item - part * M), image = (int)(part / chunks), chunk = (int)(part - (size_t)image * chunks);
+    const T* row = g + ((size_t)image * M + m) * N;
+    const int end = min(N, (chunk + 1) * ROW_SUM);
+    float sum = 0.f, v[8];
+    for (int n = chunk * ROW_SUM + lane * 8; n < end; n += 512) {
+        row_values(row + n, min(8, end - n), v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += v[e];
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    if (lane == 0) parts[part * M + m] = sum;
+}
+
+}  // namespace
+
+int product_sum_parts(const ProductParams& p, int outcome, int) {
+    int bn, wn;
+    tile_columns(product_tile(p, PRODUCT_FORWARD, outcome), &bn, &wn);
+    return p.images * ((p.N + bn - 1) / bn) * wn;
+}
+
+// Stretches of the pixels: two workgroups for every CU, each with four stages at least.  A stage is 64 pixels (fp32: 32), on the medium tile two of those.
+int product_splits(const ProductParams& p, int dtype) {
+    const int tile = product_tile(p, PRODUCT_GRAD_MATRIX, OUT_PLAIN);
+    const int bm = tile == TILE_LARGE ? 128 : 64;
+    const int step = (tile == TILE_LARGE ? 1 : 2) * (dtype == 0 ? 32 : 64);
+    const size_t tiles = tiles_of(p, false, bm, bm, 1), stages = (size_t)((p.K + step - 1) / step) * p.images;
+    size_t n = (512 + tiles - 1) / tiles;
+    if (n > stages / 4) n = stages / 4;
+    return n < 1 ? 1 : (int)n;
+}
+
+hipError_t launch_product(const ProductParams& p, int form, int outcome, int dtype, hipStream_t s) {
+    const int tile = product_tile(p, form, outcome);
+    return dtype == 0 ? launch_product_f32(p, form, outcome, tile, s)
+         : dtype == 1 ? launch_product_bf16(p, form, outcome, tile, s) : launch_product_f16(p, form, outcome, tile, s);
+}
+
+hipError_t launch_sum_parts(const float* in, void* out, int parts, size_t n, int dtype, hipStream_t s) {
+    const size_t blocks = (n + 31) / 32;
+    if (blocks * 256 >= ((size_t)1 << 32)) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks), block(256);
+    if (dtype == 0) hipLaunchKernelGGL(sum_parts_kernel<float>, grid, block, 0, s, in, (float*)out, parts, n);
+    else if (dtype == 1) hipLaunchKernelGGL(sum_parts_kernel<bf16_t>, grid, block, 0, s, in, (bf16_t*)out, parts, n);
+    else hipLaunchKernelGGL(sum_parts_kernel<f16_t>, grid, block, 0, s, in, (f16_t*)out, parts, n);
+    return hipGetLastError();
+}
+
+int row_sum_parts(int images, int, int N) { return images * ((N + ROW_SUM - 1) / ROW_SUM); }
+
+hipError_t launch_row_sums(const void* g, void* out, float* parts, int images, int M, int N, int dtype, hipStream_t s) {
+    const size_t blocks = ((size_t)row_sum_parts(images, M, N) * M + 3) / 4;
+    if (blocks * 256 >= ((size_t)1 << 32)) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks), block(256);
+    if (dtype == 0) hipLaunchKernelGGL(row_sums_kernel<float>, grid, block, 0, s, (const float*)g, parts, images, M, N);
+    else if (dtype == 1) hipLaunchKernelGGL(row_sums_kernel<bf16_t>, grid, block, 0, s, (const bf16_t*)g, parts, images, M, N);
+    else hipLaunchKernelGGL(row_sums_kernel<f16_t>, grid, block, 0, s, (const f16_t*)g, parts, images, M, N);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : launch_sum_parts(parts, out, row_sum_parts(images, M, N), (size_t)M, dtype, s);
+}
+
+}  // namespace gspn
