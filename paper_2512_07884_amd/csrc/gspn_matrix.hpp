@@ -111,6 +111,15 @@ template <typename T> __device__ __forceinline__ void row_values(const T* p, int
         for (int i = 0; i < 8; ++i) v[i] = i < n ? ldf(p + i) : 0.f;
     }
 }
+// ... for rows that end inside the eight values, out of the way of the code that all others run
+template <typename T> __device__ __forceinline__ void row_values_slow(const T* p, int n, float* v) {
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        const float x = i < n ? ldf(p + i) : 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e == i ? x : v[e];
+    }
+}
 template <typename T> __device__ __forceinline__ void row_store(T* p, int n, const float* v) {
     if (n >= 8) {
         if constexpr (sizeof(T) == 4) {

@@ -10,34 +10,74 @@ size_t tiles_of(const ProductParams& p, bool gated, int bm, int bn, int images) 
     return (size_t)((p.M + rows - 1) / rows) * ((p.N + bn - 1) / bn) * images;
 }
 
-// Large tiles where they are one for every CU or more; smaller ones, with several waves over the contracted axis, where they are not
-int product_tile(const ProductParams& p, int form, int outcome) {
+// Large tiles where they are one for every CU or more; smaller ones, with several waves over the contracted axis, where they are not.
+// 256 x 256 in 16 bits reads each operand half as often, but a CU holds one of those: where three quarters of what the CUs compute is wanted, or three fifths over a
+// long contraction.
+bool huge_tiles(const ProductParams& p, int form, bool gated, int images, int dtype) {
+    if (dtype == 0 || p.K < 512) return false;
+    const bool direct = gated ? product_direct<ProductShape<bf16_t, PRODUCT_FORWARD, OUT_GATED, 2, 2, 4, 4, 1>>(p, form, 8, 2)
+                              : product_direct<ProductShape<bf16_t, PRODUCT_FORWARD, OUT_PROJECT, 2, 2, 4, 4, 1>>(p, form, 8, 2);
+    if (!direct) return false;
+    const size_t tiles = tiles_of(p, gated, 256, 256, images), rows = (gated ? 2 : 1) * (size_t)p.M;
+    const double used = (double)rows * p.N * images / ((double)((tiles + 255) / 256) * 256 * 65536);
+    return used >= 0.75 || (used >= 0.6 && p.K >= 2048);
+}
+int product_tile(const ProductParams& p, int form, int outcome, int dtype) {
     const bool gated = outcome == OUT_GATED || outcome == OUT_GATED_GRAD;
-    if (form == PRODUCT_GRAD_MATRIX) return p.M > 64 && p.N > 64 ? TILE_LARGE : TILE_MEDIUM;
+    if (form == PRODUCT_GRAD_MATRIX) return p.M <= 64 || p.N <= 64 ? TILE_MEDIUM : (huge_tiles(p, form, false, 1, dtype) ? TILE_HUGE : TILE_LARGE);
     if (!gated && p.M <= 32 && tiles_of(p, false, 32, 128, p.images) >= 256) return TILE_FLAT;
+    if (huge_tiles(p, form, gated, p.images, dtype)) return TILE_HUGE;
     if (tiles_of(p, gated, 128, 128, p.images) >= 256) return TILE_LARGE;
     return tiles_of(p, gated, 64, 64, p.images) >= 256 ? TILE_MEDIUM : TILE_SMALL;
 }
+// a tile's side, its columns and the waves along them
 void tile_columns(int tile, int* bn, int* wn) {
-    *bn = tile == TILE_LARGE || tile == TILE_FLAT ? 128 : (tile == TILE_MEDIUM ? 64 : 32);
-    *wn = tile == TILE_FLAT ? 4 : (tile == TILE_SMALL ? 1 : 2);
+    *bn = tile == TILE_HUGE ? 256 : tile == TILE_LARGE || tile == TILE_FLAT ? 128 : (tile == TILE_MEDIUM ? 64 : 32);
+    *wn = tile == TILE_FLAT || tile == TILE_HUGE ? 4 : (tile == TILE_SMALL ? 1 : 2);
 }
 
-// 32 neighbouring results per workgroup; eight strips of the parts, added in order
-template <typename T> __global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict__ in, T* __restrict__ out, int parts, size_t n) {
-    __shared__ float strip[8][32];
+// Few parts: a thread adds those of four neighbouring results, in order
+template <typename T> __global__ void __launch_bounds__(256) sum_few_kernel(const float* __restrict__ in, T* __restrict__ out, int parts, size_t n) {
+    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    const int have = (int)min((size_t)4, n - i);
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) {
+        if (have == 4) {
+            const u32x4 v = rg_load(in + (size_t)k * n + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += __uint_as_float(v[e]);
+        } else {
+            for (int e = 0; e < have; ++e) sum[e] += in[(size_t)k * n + i + e];
+        }
+    }
+    for (int e = 0; e < have; ++e) stf(out + i + e, sum[e]);
+}
+// Many parts of few results: 32 neighbouring results per workgroup, each thread every 32nd part of one, the 32 sums added in order
+template <typename T> __global__ void __launch_bounds__(1024) sum_many_kernel(const float* __restrict__ in, T* __restrict__ out, int parts, size_t n) {
+    __shared__ float strip[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const size_t i = (size_t)blockIdx.x * 32 + x;
     float sum = 0.f;
     if (i < n)
-        for (int k = y; k < parts; k += 8) sum += in[(size_t)k * n + i];
+#pragma unroll 4
+        for (int k = y; k < parts; k += 32) sum += in[(size_t)k * n + i];
     strip[y][x] = sum;
     __syncthreads();
     if (y == 0 && i < n) {
 #pragma unroll
-        for (int k = 1; k < 8; ++k) sum += strip[k][x];
+        for (int k = 1; k < 32; ++k) sum += strip[k][x];
         stf(out + i, sum);
     }
+}
+template <typename T> hipError_t sum_parts_as(const float* in, T* out, int parts, size_t n, hipStream_t s) {
+    const bool many = parts > 16;
+    const size_t blocks = many ? (n + 31) / 32 : (n + 1023) / 1024;
+    if (blocks * 1024 >= ((size_t)1 << 32)) return hipErrorInvalidValue;
+    if (many) hipLaunchKernelGGL(sum_many_kernel<T>, dim3((unsigned)blocks), dim3(1024), 0, s, in, out, parts, n);
+    else hipLaunchKernelGGL(sum_few_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, in, out, parts, n);
+    return hipGetLastError();
 }
 
 constexpr int ROW_SUM = 4096;                          // values of a row that a wave adds
@@ -62,37 +102,30 @@ template <typename T> __global__ void __launch_bounds__(256) row_sums_kernel(con
 
 }  // namespace
 
-int product_sum_parts(const ProductParams& p, int outcome, int) {
+int product_sum_parts(const ProductParams& p, int outcome, int dtype) {
     int bn, wn;
-    tile_columns(product_tile(p, PRODUCT_FORWARD, outcome), &bn, &wn);
+    tile_columns(product_tile(p, PRODUCT_FORWARD, outcome, dtype), &bn, &wn);
     return p.images * ((p.N + bn - 1) / bn) * wn;
 }
 
-// Stretches of the pixels: two workgroups for every CU, each with four stages at least.  A stage is 64 pixels (fp32: 32), on the medium tile two of those.
+// Stretches of the pixels: two workgroups for every CU (256 x 256: one), each with six stages of 64 pixels (fp32: 32) at least
 int product_splits(const ProductParams& p, int dtype) {
-    const int tile = product_tile(p, PRODUCT_GRAD_MATRIX, OUT_PLAIN);
-    const int bm = tile == TILE_LARGE ? 128 : 64;
-    const int step = (tile == TILE_LARGE ? 1 : 2) * (dtype == 0 ? 32 : 64);
-    const size_t tiles = tiles_of(p, false, bm, bm, 1), stages = (size_t)((p.K + step - 1) / step) * p.images;
-    size_t n = (512 + tiles - 1) / tiles;
-    if (n > stages / 4) n = stages / 4;
+    const int tile = product_tile(p, PRODUCT_GRAD_MATRIX, OUT_PLAIN, dtype);
+    const int side = tile == TILE_HUGE ? 256 : (tile == TILE_LARGE ? 128 : 64), stage = dtype == 0 ? 32 : 64;
+    const size_t tiles = tiles_of(p, false, side, side, 1), stages = (size_t)((p.K + stage - 1) / stage) * p.images;
+    size_t n = tile == TILE_HUGE ? 256 / tiles : (512 + tiles / 2) / tiles;
+    if (n > stages / 6) n = stages / 6;
     return n < 1 ? 1 : (int)n;
 }
 
 hipError_t launch_product(const ProductParams& p, int form, int outcome, int dtype, hipStream_t s) {
-    const int tile = product_tile(p, form, outcome);
+    const int tile = product_tile(p, form, outcome, dtype);
     return dtype == 0 ? launch_product_f32(p, form, outcome, tile, s)
          : dtype == 1 ? launch_product_bf16(p, form, outcome, tile, s) : launch_product_f16(p, form, outcome, tile, s);
 }
 
 hipError_t launch_sum_parts(const float* in, void* out, int parts, size_t n, int dtype, hipStream_t s) {
-    const size_t blocks = (n + 31) / 32;
-    if (blocks * 256 >= ((size_t)1 << 32)) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks), block(256);
-    if (dtype == 0) hipLaunchKernelGGL(sum_parts_kernel<float>, grid, block, 0, s, in, (float*)out, parts, n);
-    else if (dtype == 1) hipLaunchKernelGGL(sum_parts_kernel<bf16_t>, grid, block, 0, s, in, (bf16_t*)out, parts, n);
-    else hipLaunchKernelGGL(sum_parts_kernel<f16_t>, grid, block, 0, s, in, (f16_t*)out, parts, n);
-    return hipGetLastError();
+    return dtype == 0 ? sum_parts_as(in, (float*)out, parts, n, s) : dtype == 1 ? sum_parts_as(in, (bf16_t*)out, parts, n, s) : sum_parts_as(in, (f16_t*)out, parts, n, s);
 }
 
 int row_sum_parts(int images, int, int N) { return images * ((N + ROW_SUM - 1) / ROW_SUM); }

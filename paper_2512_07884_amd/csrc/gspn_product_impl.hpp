@@ -19,39 +19,70 @@
 
 namespace gspn {
 
-// the activation of z, and its derivative
-template <bool GRAD> __device__ __forceinline__ float activation(float z, int act, float* slope) {
-    if (act == ACT_NONE) { if (GRAD) *slope = 1.f; return z; }
-    if (act == ACT_GELU) {
-        const float phi = fmaf(0.5f, erff(z * 0.70710678118654752f), 0.5f);
-        if (GRAD) *slope = fmaf(z * 0.39894228040143268f, __expf(-0.5f * z * z), phi);
-        return z * phi;
+// Activations of eight values, and their derivatives (one branch for all eight).
+// gelu: the normal distribution's tail 1 - Phi(a) = exp(-a^2/2) R(a) for a = |z|, where R(a) = erfcx(a / sqrt 2) / 2 falls slowly: a polynomial of degree 8 in
+// t = 1 / (1 + 0.3 a), fitted on [0, 14] for the least relative error (5.8e-8; 3.4e-7 as evaluated in fp32).  The exponential is also what
+// the derivative wants.  (With the library's erff a product of 1152 x 1152 channels on two 64x64 maps took 4 us longer.)
+template <bool GRAD> __device__ __forceinline__ float gelu(float z, float* slope) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(z), 1.f)), e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    float r = 0.0383786329f;
+    r = fmaf(r, t, -0.169167699f);
+    r = fmaf(r, t, 0.228663176f);
+    r = fmaf(r, t, -0.0765097901f);
+    r = fmaf(r, t, 0.142537644f);
+    r = fmaf(r, t, 0.094682696f);
+    r = fmaf(r, t, 0.121920534f);
+    r = fmaf(r, t, 0.119487665f);
+    r = fmaf(r, t, 7.17011553e-06f);
+    const float tail = r * e, phi = z > 0.f ? 1.f - tail : tail;
+    if (GRAD) *slope = fmaf(z * 0.39894228f, e, phi);
+    return z * phi;
+}
+// (the hardware's reciprocal: within one unit of the quotient)
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
+template <bool GRAD> __device__ __forceinline__ void activate(float* z, int act, float* slope) {
+    if (act == ACT_NONE) {
+        if (GRAD)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) slope[e] = 1.f;
+    } else if (act == ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = gelu<GRAD>(z[e], slope + e);
+    } else if (act == ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float g = logistic(z[e]);
+            z[e] *= g;
+            if (GRAD) slope[e] = fmaf(z[e], 1.f - g, g);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            z[e] = logistic(z[e]);
+            if (GRAD) slope[e] = z[e] * (1.f - z[e]);
+        }
     }
-    const float g = 1.0f / (1.0f + __expf(-z));
-    if (act == ACT_SIGMOID) { if (GRAD) *slope = g * (1.f - g); return g; }
-    if (GRAD) *slope = fmaf(z * g, 1.f - g, g);
-    return z * g;
 }
 
-// where the 16-byte piece c of row r goes in LDS: contracted axis along the row (rows of 128 bytes) ...
-__device__ __forceinline__ int along_swap(int r, int c) { return c ^ ((r >> 1) & 7); }
+// where the 16-byte piece c of row r goes in LDS: contracted axis along the row (rows of RB = 128 or 64 bytes) ...
+template <int RB> __device__ __forceinline__ int along_swap(int r, int c) { return RB == 128 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3); }
 // ... and across the rows (rows of COLS values)
 template <typename T, int COLS> __device__ __forceinline__ int across_swap(int r, int c) {
     if constexpr (sizeof(T) == 4) return COLS >= 64 ? c ^ (((r >> 3) & 1) << 3) : c;
     else return COLS >= 128 ? c ^ ((r & 3) << 2) : (COLS == 64 ? c ^ (((r >> 1) & 1) << 2) : c);
 }
 
-template <typename T> __device__ __forceinline__ MatFrag<T> along_operand(const char* tile, int r, int s, int half) {
+template <typename T, int RB> __device__ __forceinline__ MatFrag<T> along_operand(const char* tile, int r, int s, int half) {
     MatFrag<T> f;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const u32x4 a = *(const u32x4*)(tile + r * 128 + along_swap(r, 4 * s + 2 * half + j) * 16);
+            const u32x4 a = *(const u32x4*)(tile + r * RB + along_swap<RB>(r, 4 * s + 2 * half + j) * 16);
 #pragma unroll
             for (int i = 0; i < 4; ++i) f.v[4 * j + i] = __uint_as_float(a[i]);
         }
     } else {
-        f.w = *(const u32x4*)(tile + r * 128 + along_swap(r, 2 * s + half) * 16);
+        f.w = *(const u32x4*)(tile + r * RB + along_swap<RB>(r, 2 * s + half) * 16);
     }
     return f;
 }
@@ -78,25 +109,41 @@ template <typename T, int COLS> __device__ __forceinline__ MatFrag<T> across_ope
     return f;
 }
 
-template <typename T, int FORM, int OUTC, int MT, int NT, int WM, int WN, int WK>
+// 16 bytes per lane from memory to LDS without registers in between: lane l's go to `to` + 16 * l.  The request is counted like a load (vmcnt) and
+// is not known to the compiler: it writes no register, and what it writes in LDS is read behind stage_arrived() alone.
+__device__ __forceinline__ void lds_request(const void* base, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void lds_request_at(const void* at, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(at) : "memory", "m0");
+}
+// all but the `later` youngest requests of the wave have arrived, and those of the workgroup's other waves
+template <int LATER> __device__ __forceinline__ void stage_arrived() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LATER) : "memory");
+}
+__device__ const uint32_t zero_piece[4] = {0, 0, 0, 0};              // what is requested in place of positions past the end
+
+template <typename T, int FORM, int OUTC, int MT, int NT, int WM, int WN, int WK, int RB = 128, int NBUF = 2>
 struct ProductShape {
     static constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN, THREADS = 64 * WM * WN * WK;
-    static constexpr int BK = 128 / (int)sizeof(T), E = 16 / (int)sizeof(T);
-    static constexpr int A_BYTES = WK * BM * 128, B_BYTES = WK * BN * 128, STAGE = A_BYTES + B_BYTES;
+    static constexpr int BK = RB / (int)sizeof(T), E = 16 / (int)sizeof(T);
+    static constexpr int A_BYTES = WK * BM * RB, B_BYTES = WK * BN * RB, STAGE = A_BYTES + B_BYTES;
     static constexpr bool GATED = OUTC == OUT_GATED || OUTC == OUT_GATED_GRAD;
     static constexpr int PAIR = GATED ? 2 : 1;                       // row tiles that are finished together
     static constexpr int PITCH = 32 * NT + 4;                        // floats of a row of the result in LDS
-    static constexpr int FINISH = WM * WN * WK * PAIR * 32 * PITCH * 4;
-    static constexpr int LDS = 2 * STAGE > FINISH ? 2 * STAGE : FINISH;
+    static constexpr int HROWS = WK == 1 ? 16 : 32;                  // rows of a row tile that are finished together
+    static constexpr int FINISH = WM * WN * WK * PAIR * HROWS * PITCH * 4;
+    static constexpr int BUFFERS = NBUF;
+    static constexpr int LDS = BUFFERS * STAGE > FINISH ? BUFFERS * STAGE : FINISH;
     static constexpr int ROWS = GATED ? BM / 2 : BM;                 // rows of the result
 };
 
-template <typename T, int FORM, int OUTC, int MT, int NT, int WM, int WN, int WK>
+template <typename T, int FORM, int OUTC, int MT, int NT, int WM, int WN, int WK, bool DIRECT, int RB, int NBUF>
 __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const ProductParams p) {
-    using S = ProductShape<T, FORM, OUTC, MT, NT, WM, WN, WK>;
+    using S = ProductShape<T, FORM, OUTC, MT, NT, WM, WN, WK, RB, NBUF>;
     constexpr int BM = S::BM, BN = S::BN, BK = S::BK, E = S::E, THREADS = S::THREADS;
     constexpr bool A_ACROSS = FORM == PRODUCT_GRAD_INPUT, B_ACROSS = FORM != PRODUCT_GRAD_MATRIX;
-    constexpr int CA = WK * BM * 8 / THREADS, CB = WK * BN * 8 / THREADS;        // 16-byte pieces of a stage per thread
+    constexpr int PR = RB / 16, CA = WK * BM * PR / THREADS, CB = WK * BN * PR / THREADS;        // 16-byte pieces of a row; of a stage per thread
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -160,7 +207,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
                 if (ends || a_narrow) ra[i] = k0 + kk < K ? row_chunk(a + (size_t)(k0 + kk) * M, col, M) : u32x4{0, 0, 0, 0};
                 else ra[i] = rg_load(a + (size_t)(k0 + kk) * M + col);
             } else {
-                const int r = a_row(c / (8 * WK)), k = k0 + (c % (8 * WK)) * E;
+                const int r = a_row(c / (PR * WK)), k = k0 + (c % (PR * WK)) * E;
                 if (ends) ra[i] = row_chunk(a + (size_t)r * K, k, K);
                 else ra[i] = rg_load(a + (size_t)r * K + k);
             }
@@ -173,7 +220,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
                 if (ends || b_narrow) rb[i] = k0 + kk < K ? row_chunk(b + (size_t)(k0 + kk) * N, col, N) : u32x4{0, 0, 0, 0};
                 else rb[i] = rg_load(b + (size_t)(k0 + kk) * N + col);
             } else {
-                const int r = min(n0 + c / (8 * WK), N - 1), k = k0 + (c % (8 * WK)) * E;
+                const int r = min(n0 + c / (PR * WK), N - 1), k = k0 + (c % (PR * WK)) * E;
                 if (ends) rb[i] = row_chunk(b + (size_t)r * K, k, K);
                 else rb[i] = rg_load(b + (size_t)r * K + k);
             }
@@ -189,8 +236,8 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
                 const int kk = c / (BM / E), ch = c % (BM / E);
                 *(u32x4*)(ta + (size_t)kk * BM * sizeof(T) + across_swap<T, BM>(kk, ch) * 16) = ra[i];
             } else {
-                const int r = c / (8 * WK), ch = c % (8 * WK);
-                *(u32x4*)(ta + (ch >> 3) * BM * 128 + r * 128 + along_swap(r, ch & 7) * 16) = ra[i];
+                const int r = c / (PR * WK), ch = c % (PR * WK);
+                *(u32x4*)(ta + ch / PR * BM * RB + r * RB + along_swap<RB>(r, ch % PR) * 16) = ra[i];
             }
         }
 #pragma unroll
@@ -200,8 +247,8 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
                 const int kk = c / (BN / E), ch = c % (BN / E);
                 *(u32x4*)(tb + (size_t)kk * BN * sizeof(T) + across_swap<T, BN>(kk, ch) * 16) = rb[i];
             } else {
-                const int r = c / (8 * WK), ch = c % (8 * WK);
-                *(u32x4*)(tb + (ch >> 3) * BN * 128 + r * 128 + along_swap(r, ch & 7) * 16) = rb[i];
+                const int r = c / (PR * WK), ch = c % (PR * WK);
+                *(u32x4*)(tb + ch / PR * BN * RB + r * RB + along_swap<RB>(r, ch % PR) * 16) = rb[i];
             }
         }
     };
@@ -212,20 +259,20 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
 #pragma unroll
         for (int j = 0; j < NT; ++j) mat_zero(acc[i][j]);
     auto multiply = [&](int buf) {
-        const char* const ta = lds + buf * S::STAGE + wk * BM * 128;
-        const char* const tb = lds + buf * S::STAGE + S::A_BYTES + wk * BN * 128;
+        const char* const ta = lds + buf * S::STAGE + wk * BM * RB;
+        const char* const tb = lds + buf * S::STAGE + S::A_BYTES + wk * BN * RB;
 #pragma unroll
         for (int s = 0; s < BK / 16; ++s) {
             MatFrag<T> fa[MT], fb[NT];
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 if constexpr (A_ACROSS) fa[i] = across_operand<T, BM>(ta, (wm * MT + i) * 32, s, lane);
-                else fa[i] = along_operand<T>(ta, (wm * MT + i) * 32 + (lane & 31), s, half);
+                else fa[i] = along_operand<T, RB>(ta, (wm * MT + i) * 32 + (lane & 31), s, half);
             }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 if constexpr (B_ACROSS) fb[j] = across_operand<T, BN>(tb, (wn * NT + j) * 32, s, lane);
-                else fb[j] = along_operand<T>(tb, (wn * NT + j) * 32 + (lane & 31), s, half);
+                else fb[j] = along_operand<T, RB>(tb, (wn * NT + j) * 32 + (lane & 31), s, half);
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
@@ -234,7 +281,81 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
         }
     };
 
-    if (first < last) {                                              // (a split may be empty: it stores zeros)
+    if constexpr (DIRECT) {
+        // a wave requests CA (CB) kilobytes of the stage's tiles, in the order of LDS; the exchange of a row's pieces is in the addresses
+        uint32_t oa[CA], ob[CB];
+#pragma unroll
+        for (int i = 0; i < CA; ++i) {
+            const int c = (wave * CA + i) * 64 + lane;
+            if constexpr (A_ACROSS) {
+                const int kk = c / (BM / E), ch = across_swap<T, BM>(kk, c % (BM / E));
+                oa[i] = (uint32_t)(((size_t)kk * M + m0 + ch * E) * sizeof(T));
+            } else {
+                const int g = c / (BM * PR), r = c / PR % BM, ch = along_swap<RB>(r, c % PR);
+                oa[i] = (uint32_t)(((size_t)a_row(r) * K + g * BK + ch * E) * sizeof(T));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < CB; ++i) {
+            const int c = (wave * CB + i) * 64 + lane;
+            if constexpr (B_ACROSS) {
+                const int kk = c / (BN / E), ch = across_swap<T, BN>(kk, c % (BN / E));
+                ob[i] = (uint32_t)(((size_t)kk * N + n0 + ch * E) * sizeof(T));
+            } else {
+                const int g = c / (BN * PR), r = c / PR % BN, ch = along_swap<RB>(r, c % PR);
+                ob[i] = (uint32_t)(((size_t)min(n0 + r, N - 1) * K + g * BK + ch * E) * sizeof(T));
+            }
+        }
+        const uint32_t at = (uint32_t)(uintptr_t)lds_ptr(lds);
+        auto request = [&](int st, int buf) {
+            int k0 = st * STEP;
+            const T *a = A, *b = B;
+            if constexpr (FORM == PRODUCT_GRAD_MATRIX) {
+                const int im = st / stages;
+                k0 = (st - im * stages) * STEP;
+                a += (size_t)im * M * K;
+                b += (size_t)im * N * K;
+            }
+            a += A_ACROSS ? (size_t)k0 * M : (size_t)k0;
+            b += B_ACROSS ? (size_t)k0 * N : (size_t)k0;
+            const uint32_t ta = at + buf * S::STAGE + wave * CA * 1024, tb = at + buf * S::STAGE + S::A_BYTES + wave * CB * 1024;
+            if (k0 + STEP <= K) {
+#pragma unroll
+                for (int i = 0; i < CA; ++i) lds_request(a, oa[i], ta + i * 1024);
+#pragma unroll
+                for (int i = 0; i < CB; ++i) lds_request(b, ob[i], tb + i * 1024);
+            } else {
+                const int rest = K - k0;                             // positions of the stage that exist
+#pragma unroll
+                for (int i = 0; i < CA; ++i) {
+                    const int c = (wave * CA + i) * 64 + lane;
+                    const int k = A_ACROSS ? c / (BM / E) : c / (BM * PR) * BK + along_swap<RB>(c / PR % BM, c % PR) * E;
+                    lds_request_at(k < rest ? (const void*)((const char*)a + oa[i]) : zero_piece, ta + i * 1024);
+                }
+#pragma unroll
+                for (int i = 0; i < CB; ++i) {
+                    const int c = (wave * CB + i) * 64 + lane;
+                    const int k = B_ACROSS ? c / (BN / E) : c / (BN * PR) * BK + along_swap<RB>(c / PR % BN, c % PR) * E;
+                    lds_request_at(k < rest ? (const void*)((const char*)b + ob[i]) : zero_piece, tb + i * 1024);
+                }
+            }
+        };
+        if (first < last) {
+            constexpr int AHEAD = NBUF - 1;                          // stages on their way
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (first + i < last) request(first + i, i);
+            int buf = 0;
+            for (int st = first; st < last; ++st) {
+                // this stage is here, and every wave has read the one before
+                if (st + AHEAD <= last) stage_arrived<(AHEAD - 1) * (CA + CB)>();
+                else stage_arrived<0>();
+                if (st + AHEAD < last) request(st + AHEAD, buf == 0 ? NBUF - 1 : buf - 1);
+                multiply(buf);
+                buf = buf + 1 == NBUF ? 0 : buf + 1;
+            }
+        }
+    } else if (first < last) {                                       // (a split may be empty: it stores zeros)
         fetch(first);
         put(0);
         if (first + 1 < last) fetch(first + 1);
@@ -251,39 +372,66 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
     }
 
     // the result through LDS, PAIR row tiles at a time; of the WK waves that hold sums of the same results each finishes its share of the rows
-    constexpr int LANES = 4 * NT, SHARE = 32 / WK, AT_ONCE = 64 / LANES;
-    static_assert(SHARE % AT_ONCE == 0 || AT_ONCE > SHARE, "rows of a share");
-    float* const mine = (float*)lds + (size_t)wave * S::PAIR * 32 * S::PITCH;
-    const float* const from = (const float*)lds + (size_t)(wave - wk) * S::PAIR * 32 * S::PITCH;
+    constexpr int HR = S::HROWS, HALVES = 32 / HR, LANES = 4 * NT, SHARE = HR / WK, AT_ONCE = 64 / LANES, TURNS = SHARE > AT_ONCE ? SHARE / AT_ONCE : 1;
+    constexpr int BLOCKS = MT / S::PAIR * HALVES;
+    float* const mine = (float*)lds + (size_t)wave * S::PAIR * HR * S::PITCH;
+    const float* const from = (const float*)lds + (size_t)(wave - wk) * S::PAIR * HR * S::PITCH;
     const int c8 = (lane % LANES) * 8, n = n0 + wn * NT * 32 + c8, have = min(8, N - n);
     const int fresh = nt * BN - n;                                   // the first of the eight pixels that no tile before this one has
+    auto row_of = [&](int block, int turn) { return m0 + (wm * BLOCKS + block) * HR + wk * SHARE + turn * AT_ONCE + lane / LANES; };
+    const bool rows_here = AT_ONCE <= SHARE || lane / LANES < SHARE;
+    // What a row of the result is joined with is requested for all rows at once, one wait where the rows one by one would take eight
+    // (a workgroup of sixteen waves has registers for one step of the loop below at a time).
+    constexpr bool JOINS = OUTC != OUT_PLAIN;
+    constexpr int W = (int)sizeof(T) / 2;                            // 16-byte pieces of eight values
+    constexpr int HELD = !JOINS || THREADS >= 1024 ? 1 : BLOCKS;
+    u32x4 other[HELD][TURNS][W];
+    float bias[HELD][TURNS][S::PAIR];
+    const bool whole = n0 + BN <= N;                                 // (uniform) all columns of the tile exist
+    auto join = [&](int block, int to) {
 #pragma unroll
-    for (int i0 = 0; i0 < MT; i0 += S::PAIR) {
+        for (int t = 0; t < TURNS; ++t) {
+            const int m = min(row_of(block, t), M - 1);              // (rows past the end: the last one, nothing is stored)
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                other[to][t][w] = u32x4{0, 0, 0, 0};
+                if (p.extra && whole) other[to][t][w] = rg_load((const T*)p.extra + ((size_t)image * M + m) * N + n + w * E);
+            }
+#pragma unroll
+            for (int j = 0; j < S::PAIR; ++j) bias[to][t][j] = p.bias ? ldf((const T*)p.bias + (size_t)j * M + m) : 0.f;
+        }
+    };
+    if constexpr (JOINS && HELD == BLOCKS) {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) join(i, i);
+    }
+#pragma unroll
+    for (int block = 0; block < BLOCKS; ++block) {
+        constexpr bool ONE = HELD == 1;
+        if constexpr (JOINS && HELD != BLOCKS) join(block, 0);
         lds_barrier();
 #pragma unroll
         for (int i = 0; i < S::PAIR; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) mine[(i * 32 + acc_row(r, half)) * S::PITCH + j * 32 + (lane & 31)] = acc[i0 + i][j][r];
+                for (int r = 0; r < 16 / HALVES; ++r)
+                    mine[(i * HR + acc_row(r, half)) * S::PITCH + j * 32 + (lane & 31)] = acc[block / HALVES * S::PAIR + i][j][block % HALVES * 8 + r];
         lds_barrier();
-        for (int r0 = 0; r0 < SHARE; r0 += AT_ONCE) {
-            const int rr = r0 + lane / LANES, row = wk * SHARE + rr;
-            const int m = m0 + (S::GATED ? (wm * MT + i0) / 2 * 32 : (wm * MT + i0) * 32) + row;
-            const bool ok = rr < SHARE && m < M && have > 0;
+#pragma unroll
+        for (int turn = 0; turn < TURNS; ++turn) {
+            const int row = wk * SHARE + turn * AT_ONCE + lane / LANES, m = row_of(block, turn);
+            const bool ok = rows_here && m < M && have > 0;
             float v[S::PAIR][8];
 #pragma unroll
             for (int i = 0; i < S::PAIR; ++i) {
+                const float* f = from + ((size_t)i * HR + (rows_here ? row : 0)) * S::PITCH + c8;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-                if (rr < SHARE) {
+                for (int e = 0; e < 8; ++e) v[i][e] = f[e];
 #pragma unroll
-                    for (int w = 0; w < WK; ++w) {
-                        const float* f = from + ((size_t)w * S::PAIR * 32 + i * 32 + row) * S::PITCH + c8;
+                for (int w = 1; w < WK; ++w)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[i][e] += f[e];
-                    }
-                }
+                    for (int e = 0; e < 8; ++e) v[i][e] += f[(size_t)w * S::PAIR * HR * S::PITCH + e];
             }
             if constexpr (FORM == PRODUCT_GRAD_MATRIX) {
                 if (ok) {
@@ -294,33 +442,39 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
                 if (ok) row_store((T*)p.out + ((size_t)image * M + m) * N + n, have, v[0]);
             } else {
                 const size_t at = ((size_t)image * M + m) * N + n;
-                float bias[S::PAIR], x[8];
 #pragma unroll
-                for (int i = 0; i < S::PAIR; ++i) bias[i] = p.bias && ok ? ldf((const T*)p.bias + (size_t)i * M + m) : 0.f;
-                if (p.extra && ok) row_values((const T*)p.extra + at, have, x);
-                else
+                for (int i = 0; i < S::PAIR; ++i)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+                    for (int e = 0; e < 8; ++e) v[i][e] += bias[ONE ? 0 : block][turn][i];
+                float x[8];
+                if (p.extra && !whole) {
+                    if (ok) row_values_slow((const T*)p.extra + at, have, x);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = rg_elem<T>(other[ONE ? 0 : block][turn][e / E], e % E);
+                }
                 if constexpr (OUTC == OUT_PROJECT) {
+                    activate<false>(v[0], p.act, nullptr);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[0][e] = activation<false>(v[0][e] + bias[0], p.act, nullptr) + x[e];
+                    for (int e = 0; e < 8; ++e) v[0][e] += x[e];
                     if (ok) row_store((T*)p.out + at, have, v[0]);
                 } else if constexpr (OUTC == OUT_GATED) {
+                    activate<false>(v[0], p.act, nullptr);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[0][e] = activation<false>(v[0][e] + bias[0], p.act, nullptr) * (v[1][e] + bias[1]);
+                    for (int e = 0; e < 8; ++e) v[0][e] *= v[1][e];
                     if (ok) row_store((T*)p.out + at, have, v[0]);
                 } else {
                     const size_t rows = (size_t)S::PAIR * M;
+                    float slope[8];
+                    activate<true>(v[0], p.act, slope);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        float slope;
-                        const float a = activation<true>(v[0][e] + bias[0], p.act, &slope);
                         if constexpr (S::GATED) {
-                            const float u = v[1][e] + bias[1];
+                            const float a = v[0][e];
+                            v[0][e] = x[e] * v[1][e] * slope[e];
                             v[1][e] = x[e] * a;
-                            v[0][e] = x[e] * u * slope;
                         } else {
-                            v[0][e] = x[e] * slope;
+                            v[0][e] = x[e] * slope[e];
                         }
                     }
 #pragma unroll
@@ -328,11 +482,16 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
                         if (ok) row_store((T*)p.out + ((size_t)image * rows + (size_t)i * M + m) * N + n, have, v[i]);
                         if (p.sums) {
                             float sum = 0.f;
+                            if (whole && fresh <= 0) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) sum += ok && e >= fresh && e < have ? v[i][e] : 0.f;
+                                for (int e = 0; e < 8; ++e) sum += v[i][e];
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) sum += ok && e >= fresh && e < have ? v[i][e] : 0.f;
+                            }
 #pragma unroll
                             for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
-                            if (rr < SHARE && m < M && lane % LANES == 0)        // (columns past the end: 0)
+                            if (rows_here && m < M && lane % LANES == 0)         // (columns past the end: 0)
                                 p.sums[((size_t)(image * ntiles + nt) * WN + wn) * rows + (size_t)i * M + m] = sum;
                         }
                     }
@@ -343,24 +502,41 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
 }
 
 // tiles: 0: 128 x 128 (2 x 2 waves of 64 x 64); 1: 64 x 64 (two waves along the pixels, two along the stage); 2: 64 x 32 (four along the
-// stage); 3: 32 x 128 (few rows)
-enum { TILE_LARGE = 0, TILE_MEDIUM = 1, TILE_SMALL = 2, TILE_FLAT = 3 };
+// stage); 3: 32 x 128 (few rows); 4: 256 x 256 (4 x 4 waves)
+enum { TILE_LARGE = 0, TILE_MEDIUM = 1, TILE_SMALL = 2, TILE_FLAT = 3, TILE_HUGE = 4 };
 
-template <typename T, int FORM, int OUTC, int MT, int NT, int WM, int WN, int WK>
+// Requests straight to LDS: whole rows of 16-byte pieces, and offsets of 32 bits
+template <typename S> bool product_direct(const ProductParams& p, int form, int e, int width) {
+    const size_t rows = (S::GATED ? 2 : 1) * (size_t)p.M;
+    const bool a_across = form == PRODUCT_GRAD_INPUT, b_across = form != PRODUCT_GRAD_MATRIX;
+    if ((a_across && (p.M % e || p.M < S::BM)) || (b_across && (p.N % e || p.N < S::BN)) || ((!a_across || !b_across) && p.K % e)) return false;
+    const size_t step = (size_t)S::A_BYTES / (S::BM * width);        // positions of a stage
+    return (a_across ? step * p.M : rows * p.K) * width < ((size_t)1 << 32) && (b_across ? step * p.N : (size_t)p.N * p.K) * width < ((size_t)1 << 32);
+}
+
+template <typename T, int FORM, int OUTC, int MT, int NT, int WM, int WN, int WK, int RB = 128, int NBUF = 2, bool ONLY_DIRECT = false>
 hipError_t launch_product_tile(const ProductParams& p, hipStream_t s) {
-    using S = ProductShape<T, FORM, OUTC, MT, NT, WM, WN, WK>;
-    auto kernel = product_kernel<T, FORM, OUTC, MT, NT, WM, WN, WK>;
-    hipError_t e = allow_dynamic_lds((const void*)kernel, S::LDS);
+    using S = ProductShape<T, FORM, OUTC, MT, NT, WM, WN, WK, RB, NBUF>;
+    using R = ProductShape<T, FORM, OUTC, MT, NT, WM, WN, WK>;       // through registers: two buffers of whole lines
+    const bool direct = product_direct<S>(p, FORM, S::E, sizeof(T));
+    auto kernel = product_kernel<T, FORM, OUTC, MT, NT, WM, WN, WK, true, RB, NBUF>;
+    if constexpr (ONLY_DIRECT) { if (!direct) return hipErrorInvalidValue; }         // (product_tile does not choose it then)
+    else if (!direct) kernel = product_kernel<T, FORM, OUTC, MT, NT, WM, WN, WK, false, 128, 2>;
+    const int lds = direct ? S::LDS : R::LDS;
+    hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
     const size_t tiles = (size_t)((p.M + S::ROWS - 1) / S::ROWS) * ((p.N + S::BN - 1) / S::BN) * (FORM == PRODUCT_GRAD_MATRIX ? p.splits : p.images);
     if (tiles * S::THREADS >= ((size_t)1 << 32)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(S::THREADS), S::LDS, s, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(S::THREADS), lds, s, p);
     return hipGetLastError();
 }
 
 template <typename T, int FORM, int OUTC> hipError_t launch_product_as(const ProductParams& p, int tile, hipStream_t s) {
     switch (tile) {
-        case TILE_LARGE: return launch_product_tile<T, FORM, OUTC, 2, 2, 2, 2, 1>(p, s);
+        case TILE_HUGE:
+            if constexpr (sizeof(T) == 2)
+                return launch_product_tile<T, FORM, OUTC, 2, 2, 4, 4, 1, 128, 2, true>(p, s);
+        case TILE_LARGE: return launch_product_tile<T, FORM, OUTC, 2, 2, 2, 2, 1, 64, 2>(p, s);
         case TILE_MEDIUM: return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 2, 2>(p, s);
         case TILE_SMALL: return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 1, 4>(p, s);
         default:
