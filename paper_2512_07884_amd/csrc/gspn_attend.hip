@@ -5,23 +5,44 @@ namespace gspn {
 
 namespace {
 size_t rounded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
-}
 
-// 64 positions per wave where that leaves two workgroups for every CU, else 32; where that leaves less than one, the waves of a workgroup share
-// 32 positions and take the tokens apart.  Few of those workgroups and many tokens: stretches of the tokens, joined by a launch of their own.
+// The launch over the positions: 64 per wave (`can_be_wide`) where those are two thousand waves' worth, else 32.  A head's tokens stay in LDS where all of them
+// fit; four waves share up to a third of a CU's LDS, eight what is more; as many workgroups per head as fill the chip, each with equal shares of the
+// head's tiles.
+void plan_positions(AttendPlan& a, const AttendParams& p, bool can_be_wide, bool eight_waves, int row_bytes) {
+    const size_t heads = (size_t)p.B * p.heads, groups = (size_t)p.B * p.kv;
+    a.wide = can_be_wide && heads * ((p.N + 63) / 64) >= 2048;
+    const size_t tiles = (size_t)((p.N + (a.wide ? 63 : 31)) / (a.wide ? 64 : 32)) * p.per, bytes = resident_bytes(p.L, row_bytes);
+    a.resident = bytes <= (size_t)RESIDENT_MOST;
+    a.waves = a.resident && eight_waves && bytes > (size_t)RESIDENT_MOST / 3 ? 8 : 4;
+    a.lds = (int)bytes;
+    if (!a.resident) { a.workers = (int)((tiles + 3) / 4); return; }
+    const size_t fit = RESIDENT_MOST / bytes, at_once = 256 * (fit > 3 ? 3 : fit);        // workgroups that the chip holds
+    const size_t share = (at_once + groups - 1) / groups, turns = (tiles + share * a.waves - 1) / (share * a.waves);
+    a.workers = (int)((tiles + turns * a.waves - 1) / (turns * a.waves));
+}
+int steps_of(const AttendParams& p) { return (p.D + 15) / 16; }
+
+}  // namespace
+
+// Where the positions are less than three waves for every CU, the waves of a workgroup share 32 positions and take the tokens apart.  Few of those workgroups and
+// many tokens: stretches of the tokens, joined by a launch of their own.
 AttendPlan attend_plan(const AttendParams& p, int dtype) {
     AttendPlan a = {};
+    const int ks = steps_of(p), es = dtype == 0 ? 4 : 2;
     const size_t groups = (size_t)p.B * p.kv, columns = (size_t)p.per * p.N;
     a.splits = 1;
-    if (groups * ((columns + 255) / 256) >= 512) a.wide = 1;
-    else if (groups * ((columns + 127) / 128) < 256) {
-        a.by_token = 1;
-        const size_t items = groups * ((columns + 31) / 32), stages = ((size_t)p.L + 127) / 128;
-        if (items < 256 && stages > 1) {
-            size_t n = (512 + items - 1) / items;
-            if (n > (stages + 1) / 2) n = (stages + 1) / 2;
-            a.splits = (int)n;
-        }
+    if ((size_t)p.B * p.heads * ((p.N + 31) / 32) >= 768) {
+        const int dt = (ks + 1) / 2, across = es == 4 ? dt * 128 + 32 : (dt % 2 ? dt * 64 : dt * 64 + 64);
+        plan_positions(a, p, dtype != 0 && ks <= 6, true, ks * 16 * es + 16 + across);
+        return a;
+    }
+    a.few = 1;
+    const size_t items = groups * ((columns + 31) / 32), stages = ((size_t)p.L + 127) / 128;
+    if (items < 256 && stages > 1) {
+        size_t n = (512 + items - 1) / items;
+        if (n > (stages + 1) / 2) n = (stages + 1) / 2;
+        a.splits = (int)n;
     }
     if (a.splits > 1) a.bytes = rounded((size_t)a.splits * groups * (p.D + 2) * columns * sizeof(float));
     return a;
@@ -29,7 +50,9 @@ AttendPlan attend_plan(const AttendParams& p, int dtype) {
 
 AttendBackPlan attend_back_plan(const AttendParams& p, int dtype) {
     AttendBackPlan a = {};
-    a.token_waves = p.L > 64 || (dtype == 0 && p.D > 96) ? 4 : (p.L > 32 ? 2 : 1);
+    const int ks = steps_of(p);
+    plan_positions(a.q, p, dtype != 0 && ks <= 4, dtype != 0 || ks < 7, 2 * (ks * 16 * (dtype == 0 ? 4 : 2) + 16));
+    a.token_waves = p.L > 64 || (dtype == 0 && ks >= 7) ? 4 : (p.L > 32 ? 2 : 1);
     const int px = a.token_waves == 1 ? 128 : 64;
     const size_t items = (size_t)p.B * p.kv * ((p.L + 32 * a.token_waves - 1) / (32 * a.token_waves));
     const size_t stages = (size_t)((p.N + px - 1) / px) * p.per;

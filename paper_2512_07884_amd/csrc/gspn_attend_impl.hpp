@@ -27,20 +27,21 @@ __device__ __forceinline__ float other_half_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// rows of tokens in LDS: read along the row (16 bytes per lane; an odd number of 16-byte pieces: 16 rows on all banks) ...
-template <typename T, int DT> constexpr int along_pitch() { return DT * 32 * (int)sizeof(T) + 16; }
+// KS: steps of 16 channels that a head has (the last one filled with zeros), DT: tiles of 32.
+// Rows of tokens in LDS: read along the row (16 bytes per lane; an odd number of 16-byte pieces: 16 rows on all banks) ...
+template <typename T, int KS> constexpr int along_pitch() { return KS * 16 * (int)sizeof(T) + 16; }
 // ... and across the rows, turned (four rows of 64 bytes on all banks; fp32: rows four apart on both halves of the banks)
-template <typename T, int DT> constexpr int across_pitch() {
+template <typename T, int KS> constexpr int across_pitch() {
+    constexpr int DT = (KS + 1) / 2;
     return sizeof(T) == 4 ? DT * 128 + 32 : (DT % 2 ? DT * 64 : DT * 64 + 64);
 }
 
 // operand A from rows of tokens: the channels contracted (step s), row r
-template <typename T, int DT> __device__ __forceinline__ MatFrag<T> token_rows(const char* tile, int r, int s, int half) {
-    return mat_contiguous<T>(tile + r * along_pitch<T, DT>() + (16 * s + 8 * half) * (int)sizeof(T));
+template <typename T, int KS> __device__ __forceinline__ MatFrag<T> token_rows(const char* tile, int r, int s, int half) {
+    return mat_contiguous<T>(tile + r * along_pitch<T, KS>() + (16 * s + 8 * half) * (int)sizeof(T));
 }
 // ... and the tokens contracted, in the order of an accumulator's rows (16 * s ...), channels dt * 32 ...
-template <typename T, int DT> __device__ __forceinline__ MatFrag<T> token_columns(const char* tile, int dt, int s, int lane) {
-    constexpr int PITCH = across_pitch<T, DT>();
+template <typename T, int PITCH> __device__ __forceinline__ MatFrag<T> token_columns(const char* tile, int dt, int s, int lane) {
     const int half = lane >> 5;
     MatFrag<T> f;
     if constexpr (sizeof(T) == 4) {
@@ -57,32 +58,81 @@ template <typename T, int DT> __device__ __forceinline__ MatFrag<T> token_column
     return f;
 }
 
-// eight channels of a position, rows N apart, as an operand: channels d .. d + 7 at p, all of them or none
-template <typename T> __device__ __forceinline__ MatFrag<T> position_channels(const T* p, size_t N, bool have) {
+// Eight channels of positions as operands: rows N apart from `row` (the same for the whole wave) on, the lane's own offset of `at` values.  `have`: the
+// channels exist, all eight or none.
+template <typename T> __device__ __forceinline__ MatFrag<T> position_channels(const T* row, size_t N, uint32_t at, bool have) {
     MatFrag<T> f;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f.v[i] = have ? p[i * N] : 0.f;
+        for (int i = 0; i < 8; ++i) f.v[i] = have ? (row + i * N)[at] : 0.f;
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t lo = 0, hi = 0;
-            if (have) { lo = *(const uint16_t*)(p + (2 * i) * N); hi = *(const uint16_t*)(p + (2 * i + 1) * N); }
+            if (have) { lo = ((const uint16_t*)(row + (2 * i) * N))[at]; hi = ((const uint16_t*)(row + (2 * i + 1) * N))[at]; }
             f.w[i] = lo | hi << 16;
         }
     }
     return f;
+}
+// ... of two neighbouring positions with requests for both (16-bit types)
+template <typename T> __device__ __forceinline__ void position_pair_channels(const T* row, size_t N, uint32_t at, bool have, MatFrag<T>& a, MatFrag<T>& b) {
+    typedef uint32_t any4 __attribute__((aligned(2)));
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = have ? *(const any4*)((const uint16_t*)(row + i * N) + at) : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a.w[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100u);
+        b.w[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
+    }
+}
+// PT neighbouring positions n, n + 1 of a head's plane [D][N] as operands of all steps.  inside: (uniform) all positions of the wave exist; else those past
+// the end are read as the last one.
+template <typename T, int KS, int PT> __device__ __forceinline__ void load_positions(MatFrag<T> (&f)[PT][KS], const T* plane, int D, int N, int n, bool inside, int half) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        const bool have = 16 * s + 8 * half < D;
+        const T* row = plane + (size_t)(16 * s) * N;
+        const uint32_t up = 8u * half * N;
+        if constexpr (PT == 2) {
+            if (inside) { position_pair_channels<T>(row, N, up + n, have, f[0][s], f[1][s]); continue; }
+        }
+#pragma unroll
+        for (int t = 0; t < PT; ++t) f[t][s] = position_channels<T>(row, N, up + min(n + t, N - 1), have);
+    }
+}
+// ... and back: acc[t][i][r] * factor[t] to the channels of positions n, n + 1
+template <typename T, int DT, int PT> __device__ __forceinline__ void store_positions(const f32x16 (&acc)[PT][DT], const float (&factor)[PT], T* plane, int D, int N, int n, bool inside, int half) {
+    typedef uint32_t any4 __attribute__((aligned(2)));
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            T* row = plane + (size_t)(i * 32 + acc_row(r, 0)) * N;
+            const uint32_t up = 4u * half * N;
+            if (i * 32 + acc_row(r, half) < D) {
+                if constexpr (PT == 2 && sizeof(T) == 2) {
+                    if (inside) {
+                        *(any4*)((uint16_t*)row + up + n) = pack_word<T>(acc[0][i][r] * factor[0], acc[1][i][r] * factor[1]);
+                        continue;
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < PT; ++t)
+                    if (n + t < N) stf(row + up + n + t, acc[t][i][r] * factor[t]);
+            }
+        }
 }
 template <typename T> __device__ __forceinline__ float frag_value(const MatFrag<T>& f, int i) {
     if constexpr (sizeof(T) == 4) return f.v[i];
     else return rg_elem<T>(f.w, i);
 }
 
-// A stage of TB tokens on its way to LDS: keys and values of one head, and which of the tokens take part
-template <typename T, int DT, int TB> struct TokenStage {
-    static constexpr int E = 16 / (int)sizeof(T), PIECES = DT * 32 / E;            // 16-byte pieces of a token's row
-    static constexpr int COUNT = TB * PIECES / 256;                                // per thread
-    static_assert(TB * PIECES % 256 == 0, "pieces per thread");
+// A stage of TB tokens on its way to LDS through the registers of 256 threads: keys and values of one head, and which of the tokens take part
+template <typename T, int KS, int TB> struct TokenStage {
+    static constexpr int E = 16 / (int)sizeof(T), PIECES = KS * 16 / E;            // 16-byte pieces of a token's row
+    static constexpr int ALL = TB * PIECES, COUNT = (ALL + 255) / 256;             // per thread
     u32x4 k[COUNT], v[COUNT];
     uint32_t here[(TB + 63) / 64];
 
@@ -96,7 +146,7 @@ template <typename T, int DT, int TB> struct TokenStage {
         for (int i = 0; i < COUNT; ++i) {
             const int c = tid + i * 256, t = min(t0 + c / PIECES, p.L - 1), d = c % PIECES * E;
             k[i] = v[i] = u32x4{0, 0, 0, 0};
-            if (d < p.D) {
+            if (d < p.D && (ALL % 256 == 0 || c < ALL)) {
                 const size_t at = (((size_t)b * p.L + t) * p.kv + head) * p.D + d;
                 k[i] = *(const u32x4*)((const T*)p.k + at);
                 v[i] = *(const u32x4*)((const T*)p.v + at);
@@ -105,198 +155,298 @@ template <typename T, int DT, int TB> struct TokenStage {
     }
     // bits of the tokens that take part, 64 of them
     __device__ __forceinline__ uint64_t bits(int i) const { return __ballot(here[i] != 0); }
-    // ROWS of k and v into LDS at two pitches: to k_at, v_at (and k a second time to k2_at)
-    __device__ __forceinline__ void put(char* k_at, int k_pitch, char* v_at, int v_pitch, char* k2_at, int k2_pitch, int tid) const {
+    // rows of k and v into LDS, zeros for tokens that take no part
+    __device__ __forceinline__ void put(char* k_at, int k_pitch, char* v_at, int v_pitch, int tid) const {
         uint64_t w[(TB + 63) / 64];
 #pragma unroll
         for (int i = 0; i < (TB + 63) / 64; ++i) w[i] = bits(i);
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
             const int c = tid + i * 256, r = c / PIECES, o = c % PIECES * 16;
+            if (ALL % 256 && c >= ALL) break;
             const bool in = (w[TB > 64 ? r >> 6 : 0] >> (r & 63)) & 1;
             const u32x4 zero = {0, 0, 0, 0};
             *(u32x4*)(k_at + r * k_pitch + o) = in ? k[i] : zero;
             *(u32x4*)(v_at + r * v_pitch + o) = in ? v[i] : zero;
-            if (k2_at) *(u32x4*)(k2_at + r * k2_pitch + o) = in ? k[i] : zero;
         }
     }
 };
 
-// BY_TOKEN: the four waves of a workgroup hold the same 32 positions and take 32 of the 128 tokens of a stage each (few positions); else
-// each holds 32 * PT positions of its own and all take the 64 tokens of a stage.
-template <typename T, int DT, int PT, bool BY_TOKEN> struct AttendShape {
-    static constexpr int TB = BY_TOKEN ? 128 : 64;
-    static constexpr int K_BYTES = TB * along_pitch<T, DT>(), V_BYTES = TB * across_pitch<T, DT>(), STAGE = K_BYTES + V_BYTES;
-    static constexpr int BUFFERS = 2 * STAGE <= 160 * 1024 ? 2 : 1;
-    static constexpr int JOIN = BY_TOKEN ? 4 * (DT * 32 + 2) * 32 * 4 : 0;
-    static constexpr int LDS = BUFFERS * STAGE > JOIN ? BUFFERS * STAGE : JOIN;
-    static constexpr int COLUMNS = BY_TOKEN ? 32 : 128 * PT;
-};
+// All tokens of a head at once, `rows` of them (a multiple of 32; those past the end and those that take no part are zeros), and the words of 32 bits that say
+// which take part
+template <typename T, int KS, int THREADS>
+__device__ __forceinline__ void all_tokens(const AttendParams& p, int b, int head, int rows, char* k_at, int k_pitch, char* v_at, int v_pitch, uint32_t* words, int tid) {
+    constexpr int E = 16 / (int)sizeof(T), PIECES = KS * 16 / E;
+    for (int i = tid; i < ((rows + 63) & ~63); i += THREADS) {
+        const uint64_t w = __ballot(i < p.L && (!p.mask || p.mask[(size_t)b * p.L + i]));
+        if ((tid & 63) == 0) { words[i >> 5] = (uint32_t)w; words[(i >> 5) + 1] = (uint32_t)(w >> 32); }
+    }
+#pragma unroll 4
+    for (int c = tid; c < rows * PIECES; c += THREADS) {
+        const int t = c / PIECES, d = c % PIECES * E;
+        u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+        if (t < p.L && d < p.D && (!p.mask || p.mask[(size_t)b * p.L + t])) {
+            const size_t at = (((size_t)b * p.L + t) * p.kv + head) * p.D + d;
+            k = *(const u32x4*)((const T*)p.k + at);
+            v = *(const u32x4*)((const T*)p.v + at);
+        }
+        *(u32x4*)(k_at + t * k_pitch + d * (int)sizeof(T)) = k;
+        *(u32x4*)(v_at + t * v_pitch + d * (int)sizeof(T)) = v;
+    }
+}
+// accumulators that start at 0 for tokens that take part and at -inf for the others (word: bit r = token r of the 32)
+__device__ __forceinline__ void start_scores(f32x16& s, uint32_t word, int half) {
+    if (word == 0xffffffffu) { mat_zero(s); return; }
+    const uint32_t w = word >> (4 * half);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = (w >> (8 * (r >> 2) + (r & 3))) & 1 ? 0.f : -__builtin_huge_valf();
+}
 
-template <typename T, int DT, int PT, bool BY_TOKEN>
-__global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
-    using S = AttendShape<T, DT, PT, BY_TOKEN>;
-    constexpr int TB = S::TB, KS = DT * 2, TILES = BY_TOKEN ? 1 : TB / 32;
+// The running state of the wave's 32 * PT positions: output, maximum (in powers of two) and the lane's half of the sum
+template <int DT, int PT> struct AttendState {
+    f32x16 o[PT][DT];
+    float top[PT], sum[PT];
+    __device__ __forceinline__ void start() {
+#pragma unroll
+        for (int t = 0; t < PT; ++t) {
+            top[t] = -__builtin_huge_valf(); sum[t] = 0.f;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) mat_zero(o[t][i]);
+        }
+    }
+};
+// 32 tokens in LDS
+template <typename T, int KS, int PT>
+__device__ __forceinline__ void attend_tokens(const char* kt, const char* vt, uint32_t word, const MatFrag<T> (&q)[PT][KS], AttendState<(KS + 1) / 2, PT>& a, float c2, int lane) {
+    constexpr int DT = (KS + 1) / 2;
+    const int half = lane >> 5;
+    f32x16 s[PT];
+#pragma unroll
+    for (int t = 0; t < PT; ++t) start_scores(s[t], word, half);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+        const MatFrag<T> k = token_rows<T, KS>(kt, lane & 31, i, half);
+#pragma unroll
+        for (int t = 0; t < PT; ++t) mat_mul<T>(s[t], k, q[t][i]);
+    }
+#pragma unroll
+    for (int t = 0; t < PT; ++t) {
+        float m = s[t][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) m = fmaxf(m, s[t][r]);
+        m = other_half_max(m) * c2;
+        // The maximum is a reference that keeps the powers in range: it is moved only where it has grown by more than 2^8
+        if (__ballot(m > a.top[t] + 8.f)) {
+            const float next = fmaxf(a.top[t], m), shrink = next == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(a.top[t] - next);
+            a.top[t] = next;
+            a.sum[t] *= shrink;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) a.o[t][i][r] *= shrink;
+        }
+        const float ref = a.top[t] == -__builtin_huge_valf() ? 0.f : a.top[t];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) { s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c2, -ref)); a.sum[t] += s[t][r]; }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        MatFrag<T> w[PT];
+#pragma unroll
+        for (int t = 0; t < PT; ++t) {
+            float e[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) e[r] = s[t][8 * j + r];
+            w[t] = mat_from_acc<T>(e);
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const MatFrag<T> v = token_columns<T, across_pitch<T, KS>()>(vt, i, j, lane);
+#pragma unroll
+            for (int t = 0; t < PT; ++t) mat_mul<T>(a.o[t][i], v, w[t]);
+        }
+    }
+}
+__device__ __forceinline__ float attend_share(float l) { return l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l); }          // (no token: 0; NaN stays NaN)
+
+// Many positions.  A wave holds 32 * PT neighbouring positions of a head (lane and lane + 32: the same ones, other channels); PT = 2 in 16 bits reads and
+// writes the maps in words of two.
+// RESIDENT: the head's tokens stay in LDS, all of them, and each wave walks over tiles of positions without meeting the others again; 77
+// tokens of 64 channels are 32 KB.  Else stages of 64 tokens, two of them in LDS, the one after them on its way in registers, and a tile per wave.
+template <typename T, int KS, int PT, int WAVES, bool RESIDENT> struct AttendShape {
+    static constexpr int TB = 64;
+    static constexpr int K_ROW = along_pitch<T, KS>(), V_ROW = across_pitch<T, KS>(), STAGE = TB * (K_ROW + V_ROW);
+    static constexpr int BUFFERS = 2 * STAGE <= 160 * 1024 ? 2 : 1;
+    static constexpr int LDS = BUFFERS * STAGE;                      // (RESIDENT: resident_bytes)
+};
+constexpr int RESIDENT_MOST = 160 * 1024;
+inline int resident_rows(int L) { return (L + 31) & ~31; }
+inline size_t resident_bytes(int L, int row) { return (size_t)resident_rows(L) * row + (size_t)(resident_rows(L) / 32 + 2) * 4 + 8; }
+
+template <typename T, int KS, int PT, int WAVES, bool RESIDENT>
+__global__ void __launch_bounds__(64 * WAVES) attend_kernel(const AttendParams p) {
+    using S = AttendShape<T, KS, PT, WAVES, RESIDENT>;
+    constexpr int DT = (KS + 1) / 2;
+    static_assert(RESIDENT || WAVES == 4, "stages go through 256 threads");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int columns = p.per * p.N, tiles = (columns + S::COLUMNS - 1) / S::COLUMNS;
+    const int per_head = (p.N + 32 * PT - 1) / (32 * PT), tiles = per_head * p.per;
+    const unsigned item = xcd_contiguous_item(blockIdx.x, gridDim.x);
+    const int group = item / p.workers, worker = item - group * p.workers, head = group % p.kv, b = group / p.kv;
+    const float c2 = p.scale * LOG2E;
+
+    auto positions = [&](int tile, auto&& walk) {
+        const int g = tile / per_head, n = (tile - g * per_head) * 32 * PT + (lane & 31) * PT;
+        const bool inside = (tile - g * per_head + 1) * 32 * PT <= p.N;
+        const size_t plane = (size_t)b * p.heads + head * p.per + g;
+        MatFrag<T> q[PT][KS];
+        load_positions<T, KS, PT>(q, (const T*)p.q + plane * p.D * p.N, p.D, p.N, n, inside, half);
+        AttendState<DT, PT> a;
+        a.start();
+        walk(q, a);
+        float share[PT];
+#pragma unroll
+        for (int t = 0; t < PT; ++t) {
+            const float l = other_half_sum(a.sum[t]);
+            share[t] = attend_share(l);
+            if (p.lse && half == 0 && n + t < p.N) p.lse[plane * p.N + n + t] = (a.top[t] + __builtin_amdgcn_logf(l)) * LN2;
+        }
+        store_positions<T, DT, PT>(a.o, share, (T*)p.out + plane * p.D * p.N, p.D, p.N, n, inside, half);
+    };
+
+    if constexpr (RESIDENT) {
+        const int rows = (p.L + 31) & ~31;
+        char* const vt = lds + rows * S::K_ROW;
+        uint32_t* const words = (uint32_t*)(vt + rows * S::V_ROW);
+        all_tokens<T, KS, 64 * WAVES>(p, b, head, rows, lds, S::K_ROW, vt, S::V_ROW, words, tid);
+        __syncthreads();
+        for (int tile = worker * WAVES + wave; tile < tiles; tile += p.workers * WAVES)
+            positions(tile, [&](const auto& q, auto& a) {
+                for (int i = 0; i < rows / 32; ++i) {
+                    const uint32_t word = __builtin_amdgcn_readfirstlane(words[i]);
+                    if (word) attend_tokens<T, KS, PT>(lds + i * 32 * S::K_ROW, vt + i * 32 * S::V_ROW, word, q, a, c2, lane);
+                }
+            });
+    } else {
+        const int stages = (p.L + S::TB - 1) / S::TB;
+        positions(min(worker * WAVES + wave, tiles - 1), [&](const auto& q, auto& a) {       // (waves past the end: the last tile again, the same bits)
+            TokenStage<T, KS, S::TB> next;
+            next.fetch(p, b, head, 0, tid);
+            for (int st = 0; st < stages; ++st) {
+                char* const kt = lds + (S::BUFFERS == 2 ? st & 1 : 0) * S::STAGE;
+                char* const vt = kt + S::TB * S::K_ROW;
+                if (S::BUFFERS == 1 && st) lds_barrier();            // (the stage before has been read)
+                next.put(kt, S::K_ROW, vt, S::V_ROW, tid);
+                const uint64_t in = next.bits(0);
+                if (st + 1 < stages) next.fetch(p, b, head, (st + 1) * S::TB, tid);
+                lds_barrier();
+#pragma unroll
+                for (int i = 0; i < S::TB / 32; ++i) {
+                    const uint32_t word = (uint32_t)(in >> (32 * i));
+                    if (word) attend_tokens<T, KS, PT>(kt + 32 * i * S::K_ROW, vt + 32 * i * S::V_ROW, word, q, a, c2, lane);
+                }
+            }
+        });
+    }
+}
+
+// Few positions: the four waves of a workgroup hold the same 32 columns (positions of the heads that share tokens, one head after the other) and take 32 of
+// the 128 tokens of a stage each; their states meet in LDS.  Still few workgroups and many tokens: each takes a stretch of the tokens, and
+// attend_join_kernel joins the stretches.
+template <typename T, int KS> struct AttendFewShape {
+    static constexpr int TB = 128, DT = (KS + 1) / 2;
+    static constexpr int K_ROW = along_pitch<T, KS>(), V_ROW = across_pitch<T, KS>(), STAGE = TB * (K_ROW + V_ROW);
+    static constexpr int BUFFERS = 2 * STAGE <= 160 * 1024 ? 2 : 1;
+    static constexpr int JOIN = 4 * (DT * 32 + 2) * 32 * 4;
+    static constexpr int LDS = BUFFERS * STAGE > JOIN ? BUFFERS * STAGE : JOIN;
+    static constexpr bool AHEAD = sizeof(T) == 2 || KS <= 4;         // (fp32: no registers for a stage on its way beside wide heads)
+};
+template <typename T, int KS>
+__global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
+    using S = AttendFewShape<T, KS>;
+    constexpr int TB = S::TB, DT = S::DT;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int columns = p.per * p.N, tiles = (columns + 31) / 32;
     unsigned item = xcd_contiguous_item(blockIdx.x, gridDim.x);
     const int split = item % p.splits;
     item /= p.splits;
     const int tile = item % tiles, group = item / tiles, head = group % p.kv, b = group / p.kv;
     const int stages = (p.L + TB - 1) / TB;
     const int first = (int)((long)stages * split / p.splits), last = (int)((long)stages * (split + 1) / p.splits);
-
-    // the lane's positions
-    size_t base[PT];                                                // of the position's first channel
-    MatFrag<T> q[PT][KS];
-    int col[PT];
-#pragma unroll
-    for (int t = 0; t < PT; ++t) {
-        col[t] = tile * S::COLUMNS + (BY_TOKEN ? 0 : wave * 32 * PT) + t * 32 + (lane & 31);
-        const int c = min(col[t], columns - 1), g = c / p.N;
-        base[t] = ((size_t)b * p.heads + head * p.per + g) * p.D * p.N + (c - g * p.N);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const int d = 16 * s + 8 * half;
-            q[t][s] = position_channels<T>((const T*)p.q + base[t] + (size_t)d * p.N, p.N, d < p.D);
-        }
-    }
-    f32x16 o[PT][DT];
-    float top[PT], sum[PT];                                         // running maximum (in powers of two) and sum of the lane's half
-#pragma unroll
-    for (int t = 0; t < PT; ++t) {
-        top[t] = -__builtin_huge_valf(); sum[t] = 0.f;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) mat_zero(o[t][i]);
-    }
+    const size_t plane0 = (size_t)b * p.heads + head * p.per;        // the first of the heads that share the tokens
+    auto offset = [&](int column) {                                  // of a column's first channel
+        const int g = column / p.N;
+        return (uint32_t)g * p.D * p.N + (column - g * p.N);
+    };
     const float c2 = p.scale * LOG2E;
 
-    auto tokens = [&](const char* kt, const char* vt, uint32_t word) {
-        // word: bit r = token r of the 32 takes part
-        const uint32_t w = word >> (4 * half);
+    MatFrag<T> q[1][KS];
+    const uint32_t at = offset(min(tile * 32 + (lane & 31), columns - 1));
 #pragma unroll
-        for (int t = 0; t < PT; ++t) {
-            f32x16 s;
-            mat_zero(s);
-#pragma unroll
-            for (int i = 0; i < KS; ++i) mat_mul<T>(s, token_rows<T, DT>(kt, lane & 31, i, half), q[t][i]);
-            if (word != 0xffffffffu) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = (w >> (8 * (r >> 2) + (r & 3))) & 1 ? s[r] : -__builtin_huge_valf();
-            }
-            float m = s[0];
-#pragma unroll
-            for (int r = 1; r < 16; ++r) m = fmaxf(m, s[r]);
-            m = other_half_max(m) * c2;
-            // The maximum is a reference that keeps the powers in range: it is moved only where it has grown by more than 2^8
-            if (__ballot(m > top[t] + 8.f)) {
-                const float next = fmaxf(top[t], m), shrink = next == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(top[t] - next);
-                top[t] = next;
-                sum[t] *= shrink;
-#pragma unroll
-                for (int i = 0; i < DT; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[t][i][r] *= shrink;
-            }
-            const float ref = top[t] == -__builtin_huge_valf() ? 0.f : top[t];
-            float e[16];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) { e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -ref)); sum[t] += e[r]; }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const MatFrag<T> w8 = mat_from_acc<T>(e + 8 * j);
-#pragma unroll
-                for (int i = 0; i < DT; ++i) mat_mul<T>(o[t][i], token_columns<T, DT>(vt, i, j, lane), w8);
-            }
-        }
-    };
-
-    TokenStage<T, DT, TB> next;
+    for (int s = 0; s < KS; ++s)
+        q[0][s] = position_channels<T>((const T*)p.q + plane0 * p.D * p.N + (size_t)(16 * s) * p.N, p.N, at + 8u * half * p.N, 16 * s + 8 * half < p.D);
+    AttendState<DT, 1> a;
+    a.start();
     if (first < last) {
-        next.fetch(p, b, head, first * TB, tid);
+        TokenStage<T, KS, TB> next;
+        if (S::AHEAD) next.fetch(p, b, head, first * TB, tid);
         for (int st = first; st < last; ++st) {
-            const int buf = S::BUFFERS == 2 ? (st - first) & 1 : 0;
-            char* const kt = lds + buf * S::STAGE;
-            char* const vt = kt + S::K_BYTES;
+            if (!S::AHEAD) next.fetch(p, b, head, st * TB, tid);
+            char* const kt = lds + (S::BUFFERS == 2 ? (st - first) & 1 : 0) * S::STAGE;
+            char* const vt = kt + TB * S::K_ROW;
             if (S::BUFFERS == 1 && st > first) lds_barrier();       // (the stage before has been read)
-            next.put(kt, along_pitch<T, DT>(), vt, across_pitch<T, DT>(), nullptr, 0, tid);
-            uint64_t in = next.bits(0);
-            if (BY_TOKEN && wave >= 2) in = next.bits((TB + 63) / 64 - 1);
-            if (st + 1 < last) next.fetch(p, b, head, (st + 1) * TB, tid);
+            next.put(kt, S::K_ROW, vt, S::V_ROW, tid);
+            const uint64_t in = wave >= 2 ? next.bits(1) : next.bits(0);
+            if (S::AHEAD && st + 1 < last) next.fetch(p, b, head, (st + 1) * TB, tid);
             lds_barrier();
-#pragma unroll
-            for (int i = 0; i < TILES; ++i) {
-                const int r = BY_TOKEN ? wave * 32 : i * 32;
-                const uint32_t word = (uint32_t)(in >> (r & 32));
-                if (word) tokens(kt + r * along_pitch<T, DT>(), vt + r * across_pitch<T, DT>(), word);
-            }
+            const uint32_t word = (uint32_t)(in >> (wave & 1) * 32);
+            if (word) attend_tokens<T, KS, 1>(kt + wave * 32 * S::K_ROW, vt + wave * 32 * S::V_ROW, word, q, a, c2, lane);
         }
     }
-#pragma unroll
-    for (int t = 0; t < PT; ++t) sum[t] = other_half_sum(sum[t]);
+    a.sum[0] = other_half_sum(a.sum[0]);
 
-    if constexpr (BY_TOKEN) {
-        // the four waves' states meet in LDS: [wave][channel][position], then maximum and sum
-        float* const join = (float*)lds;
-        float* const tops = join + 4 * DT * 32 * 32;
-        lds_barrier();
+    // the four waves' states meet in LDS: [wave][channel][column], then maximum and sum
+    float* const join = (float*)lds;
+    float* const tops = join + 4 * DT * 32 * 32;
+    lds_barrier();
 #pragma unroll
-        for (int i = 0; i < DT; ++i)
+    for (int i = 0; i < DT; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) join[(wave * DT * 32 + i * 32 + acc_row(r, half)) * 32 + (lane & 31)] = o[0][i][r];
-        if (half == 0) { tops[wave * 32 + lane] = top[0]; tops[128 + wave * 32 + lane] = sum[0]; }
-        lds_barrier();
-        const int n = tid & 31;                                     // a thread finishes every eighth channel of a position
-        float m = tops[n], f[4], l = 0.f;
+        for (int r = 0; r < 16; ++r) join[(wave * DT * 32 + i * 32 + acc_row(r, half)) * 32 + (lane & 31)] = a.o[0][i][r];
+    if (half == 0) { tops[wave * 32 + lane] = a.top[0]; tops[128 + wave * 32 + lane] = a.sum[0]; }
+    lds_barrier();
+    const int n = tid & 31, column = tile * 32 + n;                 // a thread finishes every eighth channel of a column
+    float m = tops[n], f[4], l = 0.f;
 #pragma unroll
-        for (int w = 1; w < 4; ++w) m = fmaxf(m, tops[w * 32 + n]);
-        const float ref = m == -__builtin_huge_valf() ? 0.f : m;
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, tops[w * 32 + n]);
+    const float ref = m == -__builtin_huge_valf() ? 0.f : m;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) { f[w] = __builtin_amdgcn_exp2f(tops[w * 32 + n] - ref); l += f[w] * tops[128 + w * 32 + n]; }
-        const int column = tile * 32 + n;
-        if (column >= columns) return;
-        const int g = column / p.N;
-        const size_t at = ((size_t)b * p.heads + head * p.per + g) * p.D * p.N + (column - g * p.N);
-        if (p.splits > 1) {
-            // [split][group][channel, then maximum and sum][column]
-            float* const state = p.parts + ((size_t)split * p.B * p.kv + group) * (p.D + 2) * columns + column;
-            for (int d = tid >> 5; d < p.D; d += 8) {
-                float v = 0.f;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) v += f[w] * join[(w * DT * 32 + d) * 32 + n];
-                state[(size_t)d * columns] = v;
-            }
-            if (tid < 32) { state[(size_t)p.D * columns] = m; state[(size_t)(p.D + 1) * columns] = l; }
-            return;
-        }
-        const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);         // (NaN stays NaN)
+    for (int w = 0; w < 4; ++w) { f[w] = __builtin_amdgcn_exp2f(tops[w * 32 + n] - ref); l += f[w] * tops[128 + w * 32 + n]; }
+    if (column >= columns) return;
+    if (p.splits > 1) {
+        // [split][group][channel, then maximum and sum][column]
+        float* const state = p.parts + ((size_t)split * p.B * p.kv + group) * (p.D + 2) * columns + column;
         for (int d = tid >> 5; d < p.D; d += 8) {
             float v = 0.f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) v += f[w] * join[(w * DT * 32 + d) * 32 + n];
-            stf((T*)p.out + at + (size_t)d * p.N, v * inv);
+            state[(size_t)d * columns] = v;
         }
-        if (p.lse && tid < 32) p.lse[((size_t)b * p.heads + head * p.per + g) * p.N + (column - g * p.N)] = (m + __builtin_amdgcn_logf(l)) * LN2;
-    } else {
-#pragma unroll
-        for (int t = 0; t < PT; ++t) {
-            if (col[t] >= columns) continue;
-            const float l = sum[t], inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-#pragma unroll
-            for (int i = 0; i < DT; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int d = i * 32 + acc_row(r, half);
-                    if (d < p.D) stf((T*)p.out + base[t] + (size_t)d * p.N, o[t][i][r] * inv);
-                }
-            if (p.lse && half == 0) {
-                const int g = col[t] / p.N;
-                p.lse[((size_t)b * p.heads + head * p.per + g) * p.N + (col[t] - g * p.N)] = (top[t] + __builtin_amdgcn_logf(l)) * LN2;
-            }
-        }
+        if (tid < 32) { state[(size_t)p.D * columns] = m; state[(size_t)(p.D + 1) * columns] = l; }
+        return;
     }
+    const float share = attend_share(l);
+    T* const out = (T*)p.out + plane0 * p.D * p.N + offset(column);
+    for (int d = tid >> 5; d < p.D; d += 8) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v += f[w] * join[(w * DT * 32 + d) * 32 + n];
+        stf(out + (size_t)d * p.N, v * share);
+    }
+    if (p.lse && tid < 32) p.lse[plane0 * p.N + column] = (m + __builtin_amdgcn_logf(l)) * LN2;        // ([head][position] is the columns' own order)
 }
 
 // joins the stretches of the tokens: a thread per channel of a column
@@ -317,7 +467,7 @@ template <typename T> __global__ void __launch_bounds__(256) attend_join_kernel(
     }
     const int head = group % p.kv, b = group / p.kv, g = column / p.N;
     const size_t plane = (size_t)b * p.heads + head * p.per + g;
-    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+    const float inv = attend_share(l);
     stf((T*)p.out + (plane * p.D + d) * p.N + (column - g * p.N), v * inv);
     if (p.lse && d == 0) p.lse[plane * p.N + (column - g * p.N)] = (m + __builtin_amdgcn_logf(l)) * LN2;
 }
@@ -328,165 +478,220 @@ template <typename T> __global__ void __launch_bounds__(256) attend_join_kernel(
 // Two launches: gq (and delta) with a lane per position as in the forward call, then gk and gv with a lane per token and the positions
 // walked in stages.  p and ds are rounded to the storage type for the products, everything else is fp32.
 
-template <typename T, int DT> struct AttendGradShape {
-    static constexpr int TB = 64;
-    static constexpr int K_BYTES = TB * along_pitch<T, DT>(), K2_BYTES = TB * across_pitch<T, DT>(), STAGE = 2 * K_BYTES + K2_BYTES;
+// gq, and delta for the launch after it; positions and tokens as in attend_kernel.  Up to 64 tokens delta is the sum over the tokens, in a pass of its own
+// over what LDS holds; else the product of gout and out, which the rounding of out puts off by e: since the weights of a position add up to 1, the sum
+// of its ds is then -e, and the second launch is given delta without it.
+template <typename T, int KS, int PT, int WAVES, bool RESIDENT> struct AttendGradShape {
+    static constexpr int TB = 64, ROW = along_pitch<T, KS>(), STAGE = TB * 2 * ROW;
     static constexpr int BUFFERS = 2 * STAGE <= 160 * 1024 ? 2 : 1;
-    static constexpr int LDS = BUFFERS * STAGE;
+    static constexpr int LDS = BUFFERS * STAGE;                      // (RESIDENT: resident_bytes)
 };
-
-// gq, and delta for the launch after it.  Up to 64 tokens (one stage) delta is the sum over the tokens, in a pass of its own over what LDS holds;
-// else gout * out.
-template <typename T, int DT>
-__global__ void __launch_bounds__(256) attend_grad_q_kernel(const AttendParams p) {
-    using S = AttendGradShape<T, DT>;
-    constexpr int TB = S::TB, KS = DT * 2;
+// weights of 32 tokens, and the products of gout with their values
+template <typename T, int KS, int PT>
+__device__ __forceinline__ void attend_weights(const char* kt, const char* vt, uint32_t word, const MatFrag<T> (&q)[PT][KS], const MatFrag<T> (&go)[PT][KS],
+                                               const float (&ref)[PT], float c2, f32x16 (&e)[PT], f32x16 (&dp)[PT], int lane) {
+    const int half = lane >> 5;
+#pragma unroll
+    for (int t = 0; t < PT; ++t) { start_scores(e[t], word, half); mat_zero(dp[t]); }
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+        const MatFrag<T> k = token_rows<T, KS>(kt, lane & 31, i, half), v = token_rows<T, KS>(vt, lane & 31, i, half);
+#pragma unroll
+        for (int t = 0; t < PT; ++t) { mat_mul<T>(e[t], k, q[t][i]); mat_mul<T>(dp[t], v, go[t][i]); }
+    }
+#pragma unroll
+    for (int t = 0; t < PT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) e[t][r] = __builtin_amdgcn_exp2f(fmaf(e[t][r], c2, -ref[t]));
+}
+template <typename T, int KS, int PT, int WAVES, bool RESIDENT>
+__global__ void __launch_bounds__(64 * WAVES) attend_grad_q_kernel(const AttendParams p) {
+    using S = AttendGradShape<T, KS, PT, WAVES, RESIDENT>;
+    constexpr int DT = (KS + 1) / 2;
+    static_assert(RESIDENT || WAVES == 4, "stages go through 256 threads");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int columns = p.per * p.N, tiles = (columns + 127) / 128;
+    const int per_head = (p.N + 32 * PT - 1) / (32 * PT), tiles = per_head * p.per;
     const unsigned item = xcd_contiguous_item(blockIdx.x, gridDim.x);
-    const int tile = item % tiles, group = item / tiles, head = group % p.kv, b = group / p.kv;
-    const int stages = (p.L + TB - 1) / TB;
+    const int group = item / p.workers, worker = item - group * p.workers, head = group % p.kv, b = group / p.kv;
+    const float c2 = p.scale * LOG2E;
+    const bool few = p.L <= 64;
 
-    const int col = tile * 128 + wave * 32 + (lane & 31), c = min(col, columns - 1), g = c / p.N;
-    const size_t plane = (size_t)b * p.heads + head * p.per + g, pos = plane * p.N + (c - g * p.N);
-    const size_t base = plane * p.D * p.N + (c - g * p.N);
-    MatFrag<T> q[KS], go[KS];
-    float delta = 0.f;
+    auto positions = [&](int tile, auto&& walk) {
+        const int g = tile / per_head, n = (tile - g * per_head) * 32 * PT + (lane & 31) * PT;
+        const bool inside = (tile - g * per_head + 1) * 32 * PT <= p.N;
+        const size_t plane = (size_t)b * p.heads + head * p.per + g, at = plane * p.D * p.N;
+        MatFrag<T> q[PT][KS], go[PT][KS];
+        load_positions<T, KS, PT>(q, (const T*)p.q + at, p.D, p.N, n, inside, half);
+        load_positions<T, KS, PT>(go, (const T*)p.gout + at, p.D, p.N, n, inside, half);
+        float delta[PT], ref[PT], off[PT], scale[PT];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        const int d = 16 * s + 8 * half;
-        q[s] = position_channels<T>((const T*)p.q + base + (size_t)d * p.N, p.N, d < p.D);
-        go[s] = position_channels<T>((const T*)p.gout + base + (size_t)d * p.N, p.N, d < p.D);
-        if (stages > 1) {
-            const MatFrag<T> out = position_channels<T>((const T*)p.out + base + (size_t)d * p.N, p.N, d < p.D);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) delta = fmaf(frag_value<T>(go[s], i), frag_value<T>(out, i), delta);
+        for (int t = 0; t < PT; ++t) {
+            const float lse = p.lse[plane * p.N + min(n + t, p.N - 1)];
+            ref[t] = lse == -__builtin_huge_valf() ? __builtin_huge_valf() : lse * LOG2E;        // (no token: all weights 0)
+            delta[t] = off[t] = 0.f;
+            scale[t] = p.scale;
         }
-    }
-    delta = other_half_sum(delta);
-    const float lse = p.lse[pos], c2 = p.scale * LOG2E;
-    const float ref = lse == -__builtin_huge_valf() ? __builtin_huge_valf() : lse * LOG2E;      // (no token: all weights 0)
-
-    f32x16 acc[DT];
+        if (!few) {
 #pragma unroll
-    for (int i = 0; i < DT; ++i) mat_zero(acc[i]);
-    // weights and dp of 32 tokens
-    auto weights = [&](const char* kt, const char* vt, uint32_t word, float* e, f32x16& dp) {
-        const uint32_t w = word >> (4 * half);
-        f32x16 s;
-        mat_zero(s);
-        mat_zero(dp);
+            for (int s = 0; s < KS; ++s) {
+                MatFrag<T> out[PT][1];
+                load_positions<T, 1, PT>(out, (const T*)p.out + at + (size_t)(16 * s) * p.N, p.D - 16 * s, p.N, n, inside, half);
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            mat_mul<T>(s, token_rows<T, DT>(kt, lane & 31, i, half), q[i]);
-            mat_mul<T>(dp, token_rows<T, DT>(vt, lane & 31, i, half), go[i]);
+                for (int t = 0; t < PT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) delta[t] = fmaf(frag_value<T>(go[t][s], i), frag_value<T>(out[t][0], i), delta[t]);
+            }
+#pragma unroll
+            for (int t = 0; t < PT; ++t) delta[t] = other_half_sum(delta[t]);
         }
+        f32x16 acc[PT][DT];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) e[r] = (w >> (8 * (r >> 2) + (r & 3))) & 1 ? __builtin_amdgcn_exp2f(fmaf(s[r], c2, -ref)) : 0.f;
+        for (int t = 0; t < PT; ++t)
+#pragma unroll
+            for (int i = 0; i < DT; ++i) mat_zero(acc[t][i]);
+        // 32 tokens: towards delta, or their share of gq
+        auto sum_delta = [&](const char* kt, const char* vt, uint32_t word) {
+            f32x16 e[PT], dp[PT];
+            attend_weights<T, KS, PT>(kt, vt, word, q, go, ref, c2, e, dp, lane);
+#pragma unroll
+            for (int t = 0; t < PT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) off[t] = fmaf(e[t][r], dp[t][r], off[t]);
+        };
+        auto step = [&](const char* kt, const char* vt, uint32_t word) {
+            f32x16 e[PT], dp[PT];
+            attend_weights<T, KS, PT>(kt, vt, word, q, go, ref, c2, e, dp, lane);
+            MatFrag<T> ds[PT][2];
+#pragma unroll
+            for (int t = 0; t < PT; ++t)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float x[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) { x[r] = e[t][8 * j + r] * (dp[t][8 * j + r] - delta[t]); off[t] += x[r]; }
+                    ds[t][j] = mat_from_acc<T>(x);
+                }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+                    const MatFrag<T> k = token_columns<T, S::ROW>(kt, i, j, lane);
+#pragma unroll
+                    for (int t = 0; t < PT; ++t) mat_mul<T>(acc[t][i], k, ds[t][j]);
+                }
+        };
+        walk(sum_delta, [&] {
+#pragma unroll
+            for (int t = 0; t < PT; ++t) { delta[t] = other_half_sum(off[t]); off[t] = 0.f; }
+        }, step);
+#pragma unroll
+        for (int t = 0; t < PT; ++t) {
+            const float exact = delta[t] + other_half_sum(off[t]);
+            if (half == 0 && n + t < p.N) p.delta[plane * p.N + n + t] = exact;
+        }
+        if (p.gq) store_positions<T, DT, PT>(acc, scale, (T*)p.gq + at, p.D, p.N, n, inside, half);
     };
 
-    TokenStage<T, DT, TB> next;
-    next.fetch(p, b, head, 0, tid);
-    for (int st = 0; st < stages; ++st) {
-        const int buf = S::BUFFERS == 2 ? st & 1 : 0;
-        char* const kt = lds + buf * S::STAGE;
-        char* const vt = kt + S::K_BYTES;
-        char* const k2 = vt + S::K_BYTES;
-        if (S::BUFFERS == 1 && st) lds_barrier();
-        next.put(kt, along_pitch<T, DT>(), vt, along_pitch<T, DT>(), k2, across_pitch<T, DT>(), tid);
-        const uint64_t in = next.bits(0);
-        if (st + 1 < stages) next.fetch(p, b, head, (st + 1) * TB, tid);
-        lds_barrier();
-        if (stages == 1) {
-            float sum = 0.f;
-            for (int i = 0; i < TB / 32; ++i) {
-                const uint32_t word = (uint32_t)(in >> (32 * i));
-                if (!word) continue;
-                float e[16];
-                f32x16 dp;
-                weights(kt + 32 * i * along_pitch<T, DT>(), vt + 32 * i * along_pitch<T, DT>(), word, e, dp);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) sum = fmaf(e[r], dp[r], sum);
+    if constexpr (RESIDENT) {
+        const int rows = (p.L + 31) & ~31;
+        char* const vt = lds + rows * S::ROW;
+        uint32_t* const words = (uint32_t*)(vt + rows * S::ROW);
+        all_tokens<T, KS, 64 * WAVES>(p, b, head, rows, lds, S::ROW, vt, S::ROW, words, tid);
+        __syncthreads();
+        for (int tile = worker * WAVES + wave; tile < tiles; tile += p.workers * WAVES)
+            positions(tile, [&](auto&& sum_delta, auto&& summed, auto&& step) {
+                if (few) {
+                    for (int i = 0; i < rows / 32; ++i) {
+                        const uint32_t word = __builtin_amdgcn_readfirstlane(words[i]);
+                        if (word) sum_delta(lds + i * 32 * S::ROW, vt + i * 32 * S::ROW, word);
+                    }
+                    summed();
+                }
+                for (int i = 0; i < rows / 32; ++i) {
+                    const uint32_t word = __builtin_amdgcn_readfirstlane(words[i]);
+                    if (word) step(lds + i * 32 * S::ROW, vt + i * 32 * S::ROW, word);
+                }
+            });
+    } else {
+        const int stages = (p.L + S::TB - 1) / S::TB;
+        positions(min(worker * WAVES + wave, tiles - 1), [&](auto&&, auto&&, auto&& step) {     // (waves past the end: the last tile again, the same bits)
+            TokenStage<T, KS, S::TB> next;
+            next.fetch(p, b, head, 0, tid);
+            for (int st = 0; st < stages; ++st) {
+                char* const kt = lds + (S::BUFFERS == 2 ? st & 1 : 0) * S::STAGE;
+                char* const vt = kt + S::TB * S::ROW;
+                if (S::BUFFERS == 1 && st) lds_barrier();
+                next.put(kt, S::ROW, vt, S::ROW, tid);
+                const uint64_t in = next.bits(0);
+                if (st + 1 < stages) next.fetch(p, b, head, (st + 1) * S::TB, tid);
+                lds_barrier();
+                for (int i = 0; i < S::TB / 32; ++i) {
+                    const uint32_t word = (uint32_t)(in >> (32 * i));
+                    if (word) step(kt + 32 * i * S::ROW, vt + 32 * i * S::ROW, word);
+                }
             }
-            delta = other_half_sum(sum);
-        }
-        for (int i = 0; i < TB / 32; ++i) {
-            const uint32_t word = (uint32_t)(in >> (32 * i));
-            if (!word) continue;
-            float e[16];
-            f32x16 dp;
-            weights(kt + 32 * i * along_pitch<T, DT>(), vt + 32 * i * along_pitch<T, DT>(), word, e, dp);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) e[r] *= dp[r] - delta;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const MatFrag<T> ds = mat_from_acc<T>(e + 8 * j);
-#pragma unroll
-                for (int a = 0; a < DT; ++a) mat_mul<T>(acc[a], token_columns<T, DT>(k2 + 32 * i * across_pitch<T, DT>(), a, j, lane), ds);
-            }
-        }
+        });
     }
-    if (col >= columns) return;
-    if (half == 0) p.delta[pos] = delta;
-    if (p.gq)
-#pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int d = i * 32 + acc_row(r, half);
-                if (d < p.D) stf((T*)p.gq + base + (size_t)d * p.N, acc[i][r] * p.scale);
-            }
 }
 
 // gk and gv.  A lane is a token: WT waves of a workgroup hold 32 tokens each, 4 / WT waves the same tokens on other positions.  A stage is
 // PX positions of a head: q and gout as they are stored, [channel][position]; the scores as [position][token], so that the weights are
 // the operand of the products over the positions.
-template <typename T, int DT, int WT> struct AttendTokenShape {
-    static constexpr int WP = 4 / WT, PX = WP == 4 ? 128 : 64, PITCH = PX * (int)sizeof(T) + 16;
-    static constexpr int TILE = DT * 32 * PITCH, STAGE = 2 * TILE + 2 * PX * 4;
+// Both maps are read from LDS along the positions and across them.  16 bits: rows without gaps, their 16-byte pieces exchanged by the row's number and the
+// two halves of a piece by its bit 4, which puts the four rows of a turned request and the 32 rows of an 8-byte one on all banks.  fp32:
+// rows 16 bytes longer than their values.
+template <typename T, int KS, int WT> struct AttendTokenShape {
+    static constexpr int WP = 4 / WT, PX = WP == 4 ? 128 : 64, PITCH = PX * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : 0);
+    static constexpr int TILE = (KS + 1) / 2 * 32 * PITCH, STAGE = 2 * TILE + 2 * PX * 4;       // (rows past the channels: read, their results are not stored)
     static constexpr int BUFFERS = 2 * STAGE <= 160 * 1024 ? 2 : 1;
     static constexpr int LDS = BUFFERS * STAGE;
 };
+template <int PX> __device__ __forceinline__ int map_swap(int r) { return PX == 128 ? (r & 3) * 4 + ((r >> 2) & 3) : ((r >> 1) & 1) * 4 + ((r >> 2) & 3); }
+// byte of positions 4 * piece .. + 3 of row r (16 bits)
+template <int PX> __device__ __forceinline__ int map_piece(int r, int piece) {
+    return r * PX * 2 + (((piece >> 1) ^ map_swap<PX>(r)) << 4) + (((piece ^ (r >> 4)) & 1) << 3);
+}
 
 // operand A from [channel][position] in LDS: the positions as rows (from p0), channels contracted (step s)
-template <typename T, int PITCH> __device__ __forceinline__ MatFrag<T> map_turned(const char* tile, int p0, int s, int lane) {
+template <typename T, int PX, int PITCH> __device__ __forceinline__ MatFrag<T> map_turned(const char* tile, int p0, int s, int lane) {
     const int half = lane >> 5;
     MatFrag<T> f;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) f.v[i] = *(const float*)(tile + (16 * s + 8 * half + i) * PITCH + (p0 + (lane & 31)) * 4);
     } else {
-        const int j = lane & 15, col = p0 + (lane & 16) + (j & 3) * 4;
+        const int j = lane & 15, piece = (p0 + (lane & 16)) / 4 + (j & 3);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const u32x2 v = lds_turned(tile + (16 * s + 8 * half + 4 * i + (j >> 2)) * PITCH + col * 2);
+            const u32x2 v = lds_turned(tile + map_piece<PX>(16 * s + 8 * half + 4 * i + (j >> 2), piece));
             f.w[2 * i] = v.x; f.w[2 * i + 1] = v.y;
         }
     }
     return f;
 }
 // ... and the channels as rows (32 from dt * 32), positions contracted in the order of an accumulator's rows
-template <typename T, int PITCH> __device__ __forceinline__ MatFrag<T> map_rows(const char* tile, int dt, int p0, int j, int lane) {
-    const int half = lane >> 5;
-    const char* row = tile + (dt * 32 + (lane & 31)) * PITCH + (p0 + 16 * j + 4 * half) * (int)sizeof(T);
+template <typename T, int PX, int PITCH> __device__ __forceinline__ MatFrag<T> map_rows(const char* tile, int dt, int p0, int j, int lane) {
+    const int half = lane >> 5, r = dt * 32 + (lane & 31);
     MatFrag<T> f;
     if constexpr (sizeof(T) == 4) {
+        const char* row = tile + r * PITCH + (p0 + 16 * j + 4 * half) * 4;
         const u32x4 a = *(const u32x4*)row, b = *(const u32x4*)(row + 32);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { f.v[i] = __uint_as_float(a[i]); f.v[4 + i] = __uint_as_float(b[i]); }
     } else {
-        const u32x2 a = *(const u32x2*)row, b = *(const u32x2*)(row + 16);
+        const int piece = (p0 + 16 * j) / 4 + half;
+        const u32x2 a = *(const u32x2*)(tile + map_piece<PX>(r, piece)), b = *(const u32x2*)(tile + map_piece<PX>(r, piece + 2));
         f.w = u32x4{a.x, a.y, b.x, b.y};
     }
     return f;
 }
 
-template <typename T, int DT, int WT>
+template <typename T, int KS, int WT>
 __global__ void __launch_bounds__(256) attend_grad_tokens_kernel(const AttendParams p) {
-    using S = AttendTokenShape<T, DT, WT>;
-    constexpr int KS = DT * 2, PX = S::PX, PITCH = S::PITCH, E = 16 / (int)sizeof(T), PIECES = PX / E, COUNT = DT * 32 * PIECES / 256;
+    using S = AttendTokenShape<T, KS, WT>;
+    constexpr int DT = (KS + 1) / 2, PX = S::PX, PITCH = S::PITCH, E = 16 / (int)sizeof(T), PIECES = PX / E, ALL = KS * 16 * PIECES, COUNT = (ALL + 255) / 256;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wt = wave % WT, wp = wave / WT;
@@ -528,7 +733,7 @@ __global__ void __launch_bounds__(256) attend_grad_tokens_kernel(const AttendPar
         for (int i = 0; i < COUNT; ++i) {
             const int c = tid + i * 256, d = c / PIECES, n = n0 + c % PIECES * E;
             rq[i] = rg[i] = u32x4{0, 0, 0, 0};
-            if (d < p.D) {
+            if (d < p.D && (ALL % 256 == 0 || c < ALL)) {
                 const T* at = (const T*)p.q + (plane * p.D + d) * p.N;
                 const T* ag = (const T*)p.gout + (plane * p.D + d) * p.N;
                 if (n + E <= p.N) { rq[i] = rg_load(at + n); rg[i] = rg_load(ag + n); }
@@ -552,9 +757,17 @@ __global__ void __launch_bounds__(256) attend_grad_tokens_kernel(const AttendPar
         if (S::BUFFERS == 1 && st > first) lds_barrier();
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            const int c = tid + i * 256, d = c / PIECES, o = c % PIECES * 16;
-            *(u32x4*)(tq + d * PITCH + o) = rq[i];
-            *(u32x4*)(tg + d * PITCH + o) = rg[i];
+            const int c = tid + i * 256, d = c / PIECES;
+            if (ALL % 256 && c >= ALL) break;
+            if constexpr (sizeof(T) == 4) {
+                *(u32x4*)(tq + d * PITCH + c % PIECES * 16) = rq[i];
+                *(u32x4*)(tg + d * PITCH + c % PIECES * 16) = rg[i];
+            } else {
+                const int o = d * PITCH + ((c % PIECES ^ map_swap<PX>(d)) << 4);
+                const bool turn = d & 16;                            // the halves of the piece exchanged
+                *(u32x4*)(tq + o) = turn ? u32x4{rq[i][2], rq[i][3], rq[i][0], rq[i][1]} : rq[i];
+                *(u32x4*)(tg + o) = turn ? u32x4{rg[i][2], rg[i][3], rg[i][0], rg[i][1]} : rg[i];
+            }
         }
         if (tid < 2 * PX) tl[tid] = rl;
         if (st + 1 < last) fetch(st + 1);
@@ -565,8 +778,8 @@ __global__ void __launch_bounds__(256) attend_grad_tokens_kernel(const AttendPar
             mat_zero(dp);
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
-                mat_mul<T>(s, map_turned<T, PITCH>(tq, p0, i, lane), k[i]);
-                mat_mul<T>(dp, map_turned<T, PITCH>(tg, p0, i, lane), v[i]);
+                mat_mul<T>(s, map_turned<T, PX, PITCH>(tq, p0, i, lane), k[i]);
+                mat_mul<T>(dp, map_turned<T, PX, PITCH>(tg, p0, i, lane), v[i]);
             }
             float e[16], ds[16];
 #pragma unroll
@@ -584,8 +797,8 @@ __global__ void __launch_bounds__(256) attend_grad_tokens_kernel(const AttendPar
                 const MatFrag<T> fe = mat_from_acc<T>(e + 8 * j), fd = mat_from_acc<T>(ds + 8 * j);
 #pragma unroll
                 for (int i = 0; i < DT; ++i) {
-                    mat_mul<T>(av[i], map_rows<T, PITCH>(tg, i, p0, j, lane), fe);
-                    mat_mul<T>(ak[i], map_rows<T, PITCH>(tq, i, p0, j, lane), fd);
+                    mat_mul<T>(av[i], map_rows<T, PX, PITCH>(tg, i, p0, j, lane), fe);
+                    mat_mul<T>(ak[i], map_rows<T, PX, PITCH>(tq, i, p0, j, lane), fd);
                 }
             }
         }
@@ -618,55 +831,73 @@ __global__ void __launch_bounds__(256) attend_grad_tokens_kernel(const AttendPar
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------------
-template <typename K> hipError_t attend_launch(K kernel, size_t items, int lds, const AttendParams& p, hipStream_t s) {
-    hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
+template <typename K> hipError_t attend_launch(K kernel, size_t items, int threads, int lds, const AttendParams& p, hipStream_t s) {
+    hipError_t e = allow_dynamic_lds((const void*)kernel, RESIDENT_MOST);        // (the most that any call of it asks for)
     if (e != hipSuccess) return e;
-    if (items * 256 >= ((size_t)1 << 32)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(256), lds, s, p);
+    if (items * threads >= ((size_t)1 << 32)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(threads), lds, s, p);
     return hipGetLastError();
 }
-template <typename T, int DT, int PT, bool BY_TOKEN> hipError_t launch_attend_as(const AttendParams& p, hipStream_t s) {
-    using S = AttendShape<T, DT, PT, BY_TOKEN>;
-    const size_t tiles = ((size_t)p.per * p.N + S::COLUMNS - 1) / S::COLUMNS;
-    hipError_t e = attend_launch(attend_kernel<T, DT, PT, BY_TOKEN>, (size_t)p.B * p.kv * tiles * p.splits, S::LDS, p, s);
-    if (e != hipSuccess || p.splits == 1) return e;
-    const size_t blocks = ((size_t)p.B * p.heads * p.D * p.N + 255) / 256;
-    if (blocks * 256 >= ((size_t)1 << 32)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(attend_join_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, p);
-    return hipGetLastError();
+// Positions of a wave that can be two neighbouring ones per lane: 16 bits, and heads for whose state there are registers
+template <typename T, int KS> constexpr bool attend_wide() { return sizeof(T) == 2 && KS <= 6; }
+template <typename T, int KS> constexpr bool attend_grad_wide() { return sizeof(T) == 2 && KS <= 4; }
+
+template <typename T, int KS, int PT> hipError_t launch_attend_many(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
+    const size_t groups = (size_t)p.B * p.kv;
+    if (plan.waves == 8) return attend_launch(attend_kernel<T, KS, PT, 8, true>, groups * p.workers, 512, plan.lds, p, s);
+    if (plan.resident) return attend_launch(attend_kernel<T, KS, PT, 4, true>, groups * p.workers, 256, plan.lds, p, s);
+    return attend_launch(attend_kernel<T, KS, PT, 4, false>, groups * p.workers, 256, AttendShape<T, KS, PT, 4, false>::LDS, p, s);
 }
-template <typename T, int DT> hipError_t launch_attend_head(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
-    if (plan.by_token) return launch_attend_as<T, DT, 1, true>(p, s);
-    if constexpr (sizeof(T) == 2 || DT <= 2) { if (plan.wide) return launch_attend_as<T, DT, 2, false>(p, s); }
-    return launch_attend_as<T, DT, 1, false>(p, s);
-}
-template <typename T> hipError_t launch_attend_type(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
-    switch ((p.D + 31) / 32) {
-        case 1: return launch_attend_head<T, 1>(p, plan, s);
-        case 2: return launch_attend_head<T, 2>(p, plan, s);
-        case 3: return launch_attend_head<T, 3>(p, plan, s);
-        default: return launch_attend_head<T, 4>(p, plan, s);
+template <typename T, int KS> hipError_t launch_attend_head(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
+    if (plan.few) {
+        const size_t tiles = ((size_t)p.per * p.N + 31) / 32;
+        hipError_t e = attend_launch(attend_few_kernel<T, KS>, (size_t)p.B * p.kv * tiles * p.splits, 256, AttendFewShape<T, KS>::LDS, p, s);
+        if (e != hipSuccess || p.splits == 1) return e;
+        const size_t blocks = ((size_t)p.B * p.heads * p.D * p.N + 255) / 256;
+        if (blocks * 256 >= ((size_t)1 << 32)) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(attend_join_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, p);
+        return hipGetLastError();
     }
+    if constexpr (attend_wide<T, KS>()) { if (plan.wide) return launch_attend_many<T, KS, 2>(p, plan, s); }
+    return launch_attend_many<T, KS, 1>(p, plan, s);
 }
-template <typename T, int DT> hipError_t launch_attend_bwd_head(const AttendParams& p, const AttendBackPlan& plan, hipStream_t s) {
-    const size_t tiles = ((size_t)p.per * p.N + 127) / 128, groups = (size_t)p.B * p.kv;
-    hipError_t e = attend_launch(attend_grad_q_kernel<T, DT>, groups * tiles, AttendGradShape<T, DT>::LDS, p, s);
+template <typename T, int KS, int PT> hipError_t launch_grad_q(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
+    const size_t groups = (size_t)p.B * p.kv;
+    if constexpr (sizeof(T) == 2 || KS < 7) {                        // (registers)
+        if (plan.waves == 8) return attend_launch(attend_grad_q_kernel<T, KS, PT, 8, true>, groups * p.workers, 512, plan.lds, p, s);
+    }
+    if (plan.resident) return attend_launch(attend_grad_q_kernel<T, KS, PT, 4, true>, groups * p.workers, 256, plan.lds, p, s);
+    return attend_launch(attend_grad_q_kernel<T, KS, PT, 4, false>, groups * p.workers, 256, AttendGradShape<T, KS, PT, 4, false>::LDS, p, s);
+}
+template <typename T, int KS> hipError_t launch_attend_bwd_head(const AttendParams& p, const AttendBackPlan& plan, hipStream_t s) {
+    AttendParams q = p;
+    q.workers = plan.q.workers;
+    hipError_t e;
+    if constexpr (attend_grad_wide<T, KS>()) e = plan.q.wide ? launch_grad_q<T, KS, 2>(q, plan.q, s) : launch_grad_q<T, KS, 1>(q, plan.q, s);
+    else e = launch_grad_q<T, KS, 1>(q, plan.q, s);
     if (e != hipSuccess || (!p.gk && !p.gv)) return e;
-    const size_t items = groups * p.splits * ((p.L + 32 * plan.token_waves - 1) / (32 * plan.token_waves));
-    if constexpr (sizeof(T) == 2 || DT < 4) {                        // (fp32 heads of more than 96 channels: registers for four token waves alone)
-        if (plan.token_waves == 2) return attend_launch(attend_grad_tokens_kernel<T, DT, 2>, items, AttendTokenShape<T, DT, 2>::LDS, p, s);
-        if (plan.token_waves == 1) return attend_launch(attend_grad_tokens_kernel<T, DT, 1>, items, AttendTokenShape<T, DT, 1>::LDS, p, s);
+    const size_t items = (size_t)p.B * p.kv * p.splits * ((p.L + 32 * plan.token_waves - 1) / (32 * plan.token_waves));
+    if constexpr (sizeof(T) == 2 || KS < 7) {                        // (fp32 heads of more than 96 channels: registers for four token waves alone)
+        if (plan.token_waves == 2) return attend_launch(attend_grad_tokens_kernel<T, KS, 2>, items, 256, AttendTokenShape<T, KS, 2>::LDS, p, s);
+        if (plan.token_waves == 1) return attend_launch(attend_grad_tokens_kernel<T, KS, 1>, items, 256, AttendTokenShape<T, KS, 1>::LDS, p, s);
     }
-    return attend_launch(attend_grad_tokens_kernel<T, DT, 4>, items, AttendTokenShape<T, DT, 4>::LDS, p, s);
+    return attend_launch(attend_grad_tokens_kernel<T, KS, 4>, items, 256, AttendTokenShape<T, KS, 4>::LDS, p, s);
 }
-template <typename T> hipError_t launch_attend_bwd_type(const AttendParams& p, const AttendBackPlan& plan, hipStream_t s) {
-    switch ((p.D + 31) / 32) {
-        case 1: return launch_attend_bwd_head<T, 1>(p, plan, s);
-        case 2: return launch_attend_bwd_head<T, 2>(p, plan, s);
-        case 3: return launch_attend_bwd_head<T, 3>(p, plan, s);
-        default: return launch_attend_bwd_head<T, 4>(p, plan, s);
+// by the steps of 16 channels of a head
+#define GSPN_BY_STEPS(call)                                                                                                               \
+    switch ((p.D + 15) / 16) {                                                                                                            \
+        case 1: return call<T, 1>(p, plan, s);                                                                                            \
+        case 2: return call<T, 2>(p, plan, s);                                                                                            \
+        case 3: return call<T, 3>(p, plan, s);                                                                                            \
+        case 4: return call<T, 4>(p, plan, s);                                                                                            \
+        case 5: return call<T, 5>(p, plan, s);                                                                                            \
+        case 6: return call<T, 6>(p, plan, s);                                                                                            \
+        case 7: return call<T, 7>(p, plan, s);                                                                                            \
+        default: return call<T, 8>(p, plan, s);                                                                                           \
     }
-}
+template <typename T> hipError_t launch_attend_type(const AttendParams& p, const AttendPlan& plan, hipStream_t s) { GSPN_BY_STEPS(launch_attend_head) }
+template <typename T> hipError_t launch_attend_bwd_type(const AttendParams& p, const AttendBackPlan& plan, hipStream_t s) { GSPN_BY_STEPS(launch_attend_bwd_head) }
+#undef GSPN_BY_STEPS
 // instantiated in a translation unit per storage type
 hipError_t launch_attend_f32(const AttendParams& p, const AttendPlan& plan, hipStream_t s);
 hipError_t launch_attend_bf16(const AttendParams& p, const AttendPlan& plan, hipStream_t s);

@@ -50,12 +50,14 @@ struct AttendParams {
     int B, heads, kv, per, D, N, L;
     float scale;
     int splits;                      // stretches of the tokens (forward), of the positions (backward)
+    int workers;                     // workgroups per head of the tokens
 };
-// how a call runs: positions per wave (32 or 64), waves on the tokens instead of the positions, stretches of the tokens
-struct AttendPlan { int wide, by_token, splits; size_t bytes; };
+// How a call runs.  few: the waves of a workgroup on the tokens instead of the positions, in `splits` stretches; else: wide: 64 positions per wave instead of 32;
+// resident: a head's tokens all in LDS (`lds` bytes); waves of a workgroup; workgroups per head of the tokens.
+struct AttendPlan { int few, wide, resident, waves, workers, splits, lds; size_t bytes; };
 AttendPlan attend_plan(const AttendParams& p, int dtype);
-// backward, gk and gv: waves along the tokens (4, 2 or 1; the others along the positions), stretches of the positions
-struct AttendBackPlan { int token_waves, splits, parts; size_t delta_bytes, bytes; };
+// backward: the launch of gq; for gk and gv waves along the tokens (4, 2 or 1; the others along the positions) and stretches of the positions
+struct AttendBackPlan { AttendPlan q; int token_waves, splits, parts; size_t delta_bytes, bytes; };
 AttendBackPlan attend_back_plan(const AttendParams& p, int dtype);
 hipError_t launch_attend(const AttendParams& p, const AttendPlan& plan, int dtype, hipStream_t s);
 hipError_t launch_attend_bwd(const AttendParams& p, const AttendBackPlan& plan, int dtype, hipStream_t s);

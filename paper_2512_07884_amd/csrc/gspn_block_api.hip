@@ -100,7 +100,7 @@ int check_attend(int B, int heads, int kv_heads, int D, int H, int W, int L, flo
     if (H > GSPN_MAX_LINE || W > GSPN_MAX_LINE || D % 8 != 0 || D > GSPN_MAX_HEAD || L > GSPN_MAX_TOKENS) return GSPN_ERR_UNSUPPORTED;
     // workgroups of a launch: 32 positions each at least
     const long long N = (long long)H * W, per = heads / kv_heads;
-    if (per * N >= TOP / 4 || (long long)B * kv_heads >= TOP / 1024 || (long long)B * kv_heads * (per * N / 32 + 1) >= TOP / 128 || (long long)B * heads * N >= TOP / 16)
+    if (N >= TOP / 32 || per * N >= TOP / 4 || (long long)B * kv_heads >= TOP / 1024 || (long long)B * kv_heads * (per * N / 32 + 1) >= TOP / 128 || (long long)B * heads * N >= TOP / 16)
         return GSPN_ERR_UNSUPPORTED;
     return GSPN_OK;
 }
@@ -137,6 +137,7 @@ int gspn_cross_attention(const void* q, const void* k, const void* v, const unsi
     if (workspace && workspace_bytes < plan.bytes) return GSPN_ERR_SHAPE;
     if (!workspace) plan.splits = 1;
     p.splits = plan.splits;
+    p.workers = plan.workers;
     p.parts = (float*)workspace;
     return launch_attend(p, plan, dtype, (hipStream_t)stream) == hipSuccess ? GSPN_OK : GSPN_ERR_HIP;
 }
