@@ -9,7 +9,8 @@ size_t rounded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 // The launch over the positions: 64 per wave (`can_be_wide`) where those are two thousand waves' worth, else 32.  A head's tokens stay in LDS where all of them
 // fit; four waves share up to a third of a CU's LDS, eight what is more; as many workgroups per head as fill the chip, each with equal shares of the
 // head's tiles.
-void plan_positions(AttendPlan& a, const AttendParams& p, bool can_be_wide, bool eight_waves, int row_bytes) {
+int steps_of(const AttendParams& p) { return (p.D + 15) / 16; }
+void plan_positions(AttendPlan& a, const AttendParams& p, bool can_be_wide, bool eight_waves, int row_bytes, int (*waves)(bool, int, int), int dtype) {
     const size_t heads = (size_t)p.B * p.heads, groups = (size_t)p.B * p.kv;
     a.wide = can_be_wide && heads * ((p.N + 63) / 64) >= 2048;
     const size_t tiles = (size_t)((p.N + (a.wide ? 63 : 31)) / (a.wide ? 64 : 32)) * p.per, bytes = resident_bytes(p.L, row_bytes);
@@ -17,11 +18,12 @@ void plan_positions(AttendPlan& a, const AttendParams& p, bool can_be_wide, bool
     a.waves = a.resident && eight_waves && bytes > (size_t)RESIDENT_MOST / 3 ? 8 : 4;
     a.lds = (int)bytes;
     if (!a.resident) { a.workers = (int)((tiles + 3) / 4); return; }
-    const size_t fit = RESIDENT_MOST / bytes, at_once = 256 * (fit > 3 ? 3 : fit);        // workgroups that the chip holds
-    const size_t share = (at_once + groups - 1) / groups, turns = (tiles + share * a.waves - 1) / (share * a.waves);
+    size_t fit = RESIDENT_MOST / bytes;                              // workgroups on a CU by LDS, and by registers
+    const size_t registers = (size_t)waves(dtype == 0, steps_of(p), a.wide ? 2 : 1) * 4 / a.waves;
+    if (fit > registers) fit = registers < 1 ? 1 : registers;
+    const size_t share = (256 * fit + groups - 1) / groups, turns = (tiles + share * a.waves - 1) / (share * a.waves);
     a.workers = (int)((tiles + turns * a.waves - 1) / (turns * a.waves));
 }
-int steps_of(const AttendParams& p) { return (p.D + 15) / 16; }
 
 }  // namespace
 
@@ -34,7 +36,7 @@ AttendPlan attend_plan(const AttendParams& p, int dtype) {
     a.splits = 1;
     if ((size_t)p.B * p.heads * ((p.N + 31) / 32) >= 768) {
         const int dt = (ks + 1) / 2, across = es == 4 ? dt * 128 + 32 : (dt % 2 ? dt * 64 : dt * 64 + 64);
-        plan_positions(a, p, dtype != 0 && ks <= 6, true, ks * 16 * es + 16 + across);
+        plan_positions(a, p, dtype != 0 && ks <= 6, true, ks * 16 * es + 16 + across, attend_waves, dtype);
         return a;
     }
     a.few = 1;
@@ -51,8 +53,13 @@ AttendPlan attend_plan(const AttendParams& p, int dtype) {
 AttendBackPlan attend_back_plan(const AttendParams& p, int dtype) {
     AttendBackPlan a = {};
     const int ks = steps_of(p);
-    plan_positions(a.q, p, dtype != 0 && ks <= 4, dtype != 0 || ks < 7, 2 * (ks * 16 * (dtype == 0 ? 4 : 2) + 16));
-    a.token_waves = p.L > 64 || (dtype == 0 && ks >= 7) ? 4 : (p.L > 32 ? 2 : 1);
+    plan_positions(a.q, p, dtype != 0 && ks <= 4, dtype != 0 || ks < 7, 2 * (ks * 16 * (dtype == 0 ? 4 : 2) + 16), attend_grad_waves, dtype);
+    // waves along the tokens: as few idle ones as may be, a stage's way into LDS counted like one more
+    size_t least = ~(size_t)0;
+    for (int w = dtype == 0 && ks >= 7 ? 4 : 1; w <= 4; w *= 2) {
+        const size_t cost = (size_t)((p.L + 32 * w - 1) / (32 * w)) * (w + 1);
+        if (cost <= least) { least = cost; a.token_waves = w; }
+    }
     const int px = a.token_waves == 1 ? 128 : 64;
     const size_t items = (size_t)p.B * p.kv * ((p.L + 32 * a.token_waves - 1) / (32 * a.token_waves));
     const size_t stages = (size_t)((p.N + px - 1) / px) * p.per;
@@ -71,10 +78,11 @@ hipError_t launch_attend(const AttendParams& p, const AttendPlan& plan, int dtyp
 
 hipError_t launch_attend_bwd(const AttendParams& p, const AttendBackPlan& plan, int dtype, hipStream_t s) {
     hipError_t e = dtype == 0 ? launch_attend_bwd_f32(p, plan, s) : dtype == 1 ? launch_attend_bwd_bf16(p, plan, s) : launch_attend_bwd_f16(p, plan, s);
-    if (e != hipSuccess || plan.parts == 1) return e;
+    if (e != hipSuccess || plan.parts == 1 || (!p.gk && !p.gv)) return e;
     const size_t n = (size_t)p.B * p.L * p.kv * p.D;
-    if (p.gk && (e = launch_sum_parts(p.parts, p.gk, plan.parts, n, dtype, s)) != hipSuccess) return e;
-    return p.gv ? launch_sum_parts(p.parts + (size_t)plan.parts * n, p.gv, plan.parts, n, dtype, s) : e;
+    const float* const gv = p.parts + (size_t)plan.parts * n;
+    if (!p.gk) return launch_sum_parts(gv, p.gv, plan.parts, n, dtype, s);
+    return launch_sum_parts(p.parts, p.gk, plan.parts, n, dtype, s, p.gv ? gv : nullptr, p.gv);
 }
 
 }  // namespace gspn

@@ -280,11 +280,17 @@ template <typename T, int KS, int PT, int WAVES, bool RESIDENT> struct AttendSha
     static constexpr int LDS = BUFFERS * STAGE;                      // (RESIDENT: resident_bytes)
 };
 constexpr int RESIDENT_MOST = 160 * 1024;
+// Waves per SIMD that the kernels' registers leave room for, by which a call's workgroups are counted too.  (From two on a wave has 256 registers
+// of one file, none in the accumulation file that takes a move per value read.)
+constexpr int attend_waves(bool f32, int ks, int pt) { return f32 ? (ks <= 4 ? 4 : ks <= 6 ? 3 : 2) : pt == 1 ? (ks <= 6 ? 4 : 3) : (ks <= 2 ? 4 : ks <= 4 ? 3 : 2); }
+constexpr int attend_grad_waves(bool f32, int ks, int pt) {
+    return f32 ? (ks <= 2 ? 4 : ks <= 4 ? 3 : ks <= 7 ? 2 : 1) : pt == 1 ? (ks <= 3 ? 4 : ks <= 6 ? 3 : 2) : (ks <= 2 ? 3 : 2);
+}
 inline int resident_rows(int L) { return (L + 31) & ~31; }
 inline size_t resident_bytes(int L, int row) { return (size_t)resident_rows(L) * row + (size_t)(resident_rows(L) / 32 + 2) * 4 + 8; }
 
 template <typename T, int KS, int PT, int WAVES, bool RESIDENT>
-__global__ void __launch_bounds__(64 * WAVES) attend_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_waves(sizeof(T) == 4, KS, PT) : ((sizeof(T) == 2 ? PT == 1 || KS <= 4 : KS <= 6) ? 2 : 1)) attend_kernel(const AttendParams p) {
     using S = AttendShape<T, KS, PT, WAVES, RESIDENT>;
     constexpr int DT = (KS + 1) / 2;
     static_assert(RESIDENT || WAVES == 4, "stages go through 256 threads");
@@ -363,7 +369,7 @@ template <typename T, int KS> struct AttendFewShape {
     static constexpr bool AHEAD = sizeof(T) == 2 || KS <= 4;         // (fp32: no registers for a stage on its way beside wide heads)
 };
 template <typename T, int KS>
-__global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS <= 5 : KS <= 4) ? 2 : 1) attend_few_kernel(const AttendParams p) {
     using S = AttendFewShape<T, KS>;
     constexpr int TB = S::TB, DT = S::DT;
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -449,26 +455,47 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
     if (p.lse && tid < 32) p.lse[plane0 * p.N + column] = (m + __builtin_amdgcn_logf(l)) * LN2;        // ([head][position] is the columns' own order)
 }
 
-// joins the stretches of the tokens: a thread per channel of a column
+// Joins the stretches of the tokens: 32 columns of a group and eight channels per workgroup.  The stretches' factors are worked out once per workgroup (eight threads
+// per column) and shared; a thread then adds one channel of a column over them.
 template <typename T> __global__ void __launch_bounds__(256) attend_join_kernel(const AttendParams p) {
-    const int columns = p.per * p.N;
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, groups = (size_t)p.B * p.kv;
-    if (i >= groups * p.D * columns) return;
-    const int column = i % columns, d = (i / columns) % p.D;
-    const size_t group = i / columns / p.D, step = groups * (p.D + 2) * columns;
-    const float* state = p.parts + group * (p.D + 2) * columns + column;
-    float m = -__builtin_huge_valf(), l = 0.f, v = 0.f;
-    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, state[s * step + (size_t)p.D * columns]);
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    float* const factor = (float*)lds;                               // [split][column]
+    float* const strip = factor + p.splits * 32;                     // [8][column]
+    const int columns = p.per * p.N, tiles = (columns + 31) / 32, slices = (p.D + 7) / 8;
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const unsigned tile = blockIdx.x % tiles, slice = blockIdx.x / tiles % slices, group = blockIdx.x / tiles / slices;
+    const int column = tile * 32 + x, c = min(column, columns - 1), d = slice * 8 + y;
+    const size_t step = (size_t)p.B * p.kv * (p.D + 2) * columns;
+    const float* const state = p.parts + (size_t)group * (p.D + 2) * columns + c;
+    float m = -__builtin_huge_valf();
+#pragma unroll 4
+    for (int s = y; s < p.splits; s += 8) m = fmaxf(m, state[s * step + (size_t)p.D * columns]);
+    strip[y * 32 + x] = m;
+    __syncthreads();
+    m = strip[x];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) m = fmaxf(m, strip[i * 32 + x]);
+    __syncthreads();
     const float ref = m == -__builtin_huge_valf() ? 0.f : m;
-    for (int s = 0; s < p.splits; ++s) {
+    float l = 0.f;
+#pragma unroll 4
+    for (int s = y; s < p.splits; s += 8) {
         const float f = __builtin_amdgcn_exp2f(state[s * step + (size_t)p.D * columns] - ref);
-        l += f * state[s * step + (size_t)(p.D + 1) * columns];
-        v += f * state[s * step + (size_t)d * columns];
+        factor[s * 32 + x] = f;
+        l = fmaf(f, state[s * step + (size_t)(p.D + 1) * columns], l);
     }
+    strip[y * 32 + x] = l;
+    __syncthreads();
+    l = strip[x];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) l += strip[i * 32 + x];
+    if (column >= columns || d >= p.D) return;
+    float v = 0.f;
+#pragma unroll 8
+    for (int s = 0; s < p.splits; ++s) v = fmaf(factor[s * 32 + x], state[s * step + (size_t)d * columns], v);
     const int head = group % p.kv, b = group / p.kv, g = column / p.N;
     const size_t plane = (size_t)b * p.heads + head * p.per + g;
-    const float inv = attend_share(l);
-    stf((T*)p.out + (plane * p.D + d) * p.N + (column - g * p.N), v * inv);
+    stf((T*)p.out + (plane * p.D + d) * p.N + (column - g * p.N), v * attend_share(l));
     if (p.lse && d == 0) p.lse[plane * p.N + (column - g * p.N)] = (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
@@ -505,7 +532,7 @@ __device__ __forceinline__ void attend_weights(const char* kt, const char* vt, u
         for (int r = 0; r < 16; ++r) e[t][r] = __builtin_amdgcn_exp2f(fmaf(e[t][r], c2, -ref[t]));
 }
 template <typename T, int KS, int PT, int WAVES, bool RESIDENT>
-__global__ void __launch_bounds__(64 * WAVES) attend_grad_q_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_grad_waves(sizeof(T) == 4, KS, PT) : ((sizeof(T) == 2 ? KS < 8 && (PT == 1 || KS < 4) : KS <= 4) ? 2 : 1)) attend_grad_q_kernel(const AttendParams p) {
     using S = AttendGradShape<T, KS, PT, WAVES, RESIDENT>;
     constexpr int DT = (KS + 1) / 2;
     static_assert(RESIDENT || WAVES == 4, "stages go through 256 threads");
@@ -689,7 +716,7 @@ template <typename T, int PX, int PITCH> __device__ __forceinline__ MatFrag<T> m
 }
 
 template <typename T, int KS, int WT>
-__global__ void __launch_bounds__(256) attend_grad_tokens_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS < 5 || (KS == 5 && WT > 1) : KS <= 3) ? 2 : 1) attend_grad_tokens_kernel(const AttendParams p) {
     using S = AttendTokenShape<T, KS, WT>;
     constexpr int DT = (KS + 1) / 2, PX = S::PX, PITCH = S::PITCH, E = 16 / (int)sizeof(T), PIECES = PX / E, ALL = KS * 16 * PIECES, COUNT = (ALL + 255) / 256;
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -704,6 +731,7 @@ __global__ void __launch_bounds__(256) attend_grad_tokens_kernel(const AttendPar
     // the lane's token
     const int token = tt * 32 * WT + wt * 32 + (lane & 31);
     const bool in = token < p.L && (!p.mask || p.mask[(size_t)b * p.L + token]);
+    const bool some = __ballot(in) != 0;                             // (of the wave's tokens; else it only helps to bring the stages)
     const size_t row = (((size_t)b * p.L + min(token, p.L - 1)) * p.kv + head) * p.D;
     MatFrag<T> k[KS], v[KS];
 #pragma unroll
@@ -772,7 +800,8 @@ __global__ void __launch_bounds__(256) attend_grad_tokens_kernel(const AttendPar
         if (tid < 2 * PX) tl[tid] = rl;
         if (st + 1 < last) fetch(st + 1);
         lds_barrier();
-        for (int p0 = wp * 32; p0 < PX; p0 += 32 * S::WP) {
+#pragma unroll 1
+        for (int p0 = some ? wp * 32 : PX; p0 < PX; p0 += 32 * S::WP) {
             f32x16 s, dp;
             mat_zero(s);
             mat_zero(dp);
@@ -853,10 +882,7 @@ template <typename T, int KS> hipError_t launch_attend_head(const AttendParams& 
         const size_t tiles = ((size_t)p.per * p.N + 31) / 32;
         hipError_t e = attend_launch(attend_few_kernel<T, KS>, (size_t)p.B * p.kv * tiles * p.splits, 256, AttendFewShape<T, KS>::LDS, p, s);
         if (e != hipSuccess || p.splits == 1) return e;
-        const size_t blocks = ((size_t)p.B * p.heads * p.D * p.N + 255) / 256;
-        if (blocks * 256 >= ((size_t)1 << 32)) return hipErrorInvalidValue;
-        hipLaunchKernelGGL(attend_join_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, p);
-        return hipGetLastError();
+        return attend_launch(attend_join_kernel<T>, (size_t)p.B * p.kv * tiles * ((p.D + 7) / 8), 256, (p.splits + 8) * 32 * 4, p, s);
     }
     if constexpr (attend_wide<T, KS>()) { if (plan.wide) return launch_attend_many<T, KS, 2>(p, plan, s); }
     return launch_attend_many<T, KS, 1>(p, plan, s);

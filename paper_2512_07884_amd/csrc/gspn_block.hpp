@@ -30,8 +30,8 @@ struct ProductParams {
 int product_sum_parts(const ProductParams& p, int outcome, int dtype);
 int product_splits(const ProductParams& p, int dtype);            // PRODUCT_GRAD_MATRIX: stretches that such a call is cut into
 hipError_t launch_product(const ProductParams& p, int form, int outcome, int dtype, hipStream_t s);
-// out[i] = sum over `parts` of in[part][i], in order, rounded to the storage type
-hipError_t launch_sum_parts(const float* in, void* out, int parts, size_t n, int dtype, hipStream_t s);
+// out[i] = sum over `parts` of in[part][i], in order, rounded to the storage type; and a second sum of the same size in the same launch
+hipError_t launch_sum_parts(const float* in, void* out, int parts, size_t n, int dtype, hipStream_t s, const float* in2 = nullptr, void* out2 = nullptr);
 // out[m] = sum over images and pixels of g[image][m][n]
 hipError_t launch_row_sums(const void* g, void* out, float* parts, int images, int M, int N, int dtype, hipStream_t s);
 int row_sum_parts(int images, int M, int N);

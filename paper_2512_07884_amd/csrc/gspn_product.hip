@@ -37,7 +37,8 @@ void tile_columns(int tile, int* bn, int* wn) {
 }
 
 // Few parts: a thread adds those of four neighbouring results, in order
-template <typename T> __global__ void __launch_bounds__(256) sum_few_kernel(const float* __restrict__ in, T* __restrict__ out, int parts, size_t n) {
+template <typename T> __global__ void __launch_bounds__(256) sum_few_kernel(const float* __restrict__ in, T* __restrict__ out, int parts, size_t n, const float* __restrict__ in2, T* __restrict__ out2) {
+    if (blockIdx.y) { in = in2; out = out2; }
     const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= n) return;
     const int have = (int)min((size_t)4, n - i);
@@ -55,7 +56,8 @@ template <typename T> __global__ void __launch_bounds__(256) sum_few_kernel(cons
     for (int e = 0; e < have; ++e) stf(out + i + e, sum[e]);
 }
 // Many parts of few results: 32 neighbouring results per workgroup, each thread every 32nd part of one, the 32 sums added in order
-template <typename T> __global__ void __launch_bounds__(1024) sum_many_kernel(const float* __restrict__ in, T* __restrict__ out, int parts, size_t n) {
+template <typename T> __global__ void __launch_bounds__(1024) sum_many_kernel(const float* __restrict__ in, T* __restrict__ out, int parts, size_t n, const float* __restrict__ in2, T* __restrict__ out2) {
+    if (blockIdx.y) { in = in2; out = out2; }
     __shared__ float strip[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const size_t i = (size_t)blockIdx.x * 32 + x;
@@ -71,12 +73,14 @@ template <typename T> __global__ void __launch_bounds__(1024) sum_many_kernel(co
         stf(out + i, sum);
     }
 }
-template <typename T> hipError_t sum_parts_as(const float* in, T* out, int parts, size_t n, hipStream_t s) {
+template <typename T> hipError_t sum_parts_as(const float* in, void* out_, int parts, size_t n, hipStream_t s, const float* in2, void* out2_) {
+    T *const out = (T*)out_, *const out2 = (T*)out2_;
+    const unsigned sums = out2 ? 2 : 1;
     const bool many = parts > 16;
     const size_t blocks = many ? (n + 31) / 32 : (n + 1023) / 1024;
     if (blocks * 1024 >= ((size_t)1 << 32)) return hipErrorInvalidValue;
-    if (many) hipLaunchKernelGGL(sum_many_kernel<T>, dim3((unsigned)blocks), dim3(1024), 0, s, in, out, parts, n);
-    else hipLaunchKernelGGL(sum_few_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, in, out, parts, n);
+    if (many) hipLaunchKernelGGL(sum_many_kernel<T>, dim3((unsigned)blocks, sums), dim3(1024), 0, s, in, out, parts, n, in2, out2);
+    else hipLaunchKernelGGL(sum_few_kernel<T>, dim3((unsigned)blocks, sums), dim3(256), 0, s, in, out, parts, n, in2, out2);
     return hipGetLastError();
 }
 
@@ -124,8 +128,9 @@ hipError_t launch_product(const ProductParams& p, int form, int outcome, int dty
          : dtype == 1 ? launch_product_bf16(p, form, outcome, tile, s) : launch_product_f16(p, form, outcome, tile, s);
 }
 
-hipError_t launch_sum_parts(const float* in, void* out, int parts, size_t n, int dtype, hipStream_t s) {
-    return dtype == 0 ? sum_parts_as(in, (float*)out, parts, n, s) : dtype == 1 ? sum_parts_as(in, (bf16_t*)out, parts, n, s) : sum_parts_as(in, (f16_t*)out, parts, n, s);
+hipError_t launch_sum_parts(const float* in, void* out, int parts, size_t n, int dtype, hipStream_t s, const float* in2, void* out2) {
+    return dtype == 0 ? sum_parts_as<float>(in, out, parts, n, s, in2, out2)
+         : dtype == 1 ? sum_parts_as<bf16_t>(in, out, parts, n, s, in2, out2) : sum_parts_as<f16_t>(in, out, parts, n, s, in2, out2);
 }
 
 int row_sum_parts(int images, int, int N) { return images * ((N + ROW_SUM - 1) / ROW_SUM); }
