@@ -70,9 +70,6 @@ SPILL_ALLOWED = {
     # any-size kernel, reverse sweep in 16-bit storage: 128 registers, so that sixteen waves share a CU; what the loading waves park
     # (at most 14 values in bf16, 8 in fp16) lies between the chunks, none in the line loops
     "ragged_kernelItLi2": 14, "ragged_kernelINS_5f16_tELi2": 8,
-    # cross attention, two positions per lane, heads of 49 to 64 channels, tokens resident: three waves per SIMD in 168 registers with four
-    # values in scratch memory, outside the loop over the tokens (77 tokens on two 128x128 latents 49 -> 45 us); parity-tested in bf16 and fp16
-    "attend_kernelItLi4ELi2ELi4ELb1": 4, "attend_kernelINS_5f16_tELi4ELi2ELi4ELb1": 4,
     # fp32 maps with rows of 112 bytes on workgroups of more than four waves, without h_save: off every benchmark shape
     # (the plane kernel takes 28x28, the four-wave instantiation 56x56); kept because the shapes must run somewhere
     "fwd_tile_kernelIfLi2ELi1ELi28ELb0ELi8ELb0ELi8ELb0ELb0ELb0": 259, "fwd_tile_kernelIfLi2ELi1ELi28ELb0ELi8ELb0ELi8ELb1ELb0ELb0": 47,

@@ -6,21 +6,24 @@ namespace gspn {
 namespace {
 size_t rounded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
-// The launch over the positions: 64 per wave (`can_be_wide`) where those are two thousand waves' worth, else 32.  A head's tokens stay in LDS where all of them
-// fit; four waves share up to a third of a CU's LDS, eight what is more; as many workgroups per head as fill the chip, each with equal shares of the
-// head's tiles.
 int steps_of(const AttendParams& p) { return (p.D + 15) / 16; }
-void plan_positions(AttendPlan& a, const AttendParams& p, bool can_be_wide, bool eight_waves, int row_bytes, int (*waves)(bool, int, int), int dtype) {
-    const size_t heads = (size_t)p.B * p.heads, groups = (size_t)p.B * p.kv;
-    a.wide = can_be_wide && heads * ((p.N + 63) / 64) >= 2048;
-    const size_t tiles = (size_t)((p.N + (a.wide ? 63 : 31)) / (a.wide ? 64 : 32)) * p.per, bytes = resident_bytes(p.L, row_bytes);
+// The launch over the positions, 32 per wave.  A head's tokens stay in LDS where all of them fit; four waves share up to a third of a CU's LDS, eight what is
+// more; as many workgroups per head as fill the chip (by LDS, and by `simd` waves per SIMD), each with equal shares of the head's tiles.
+void plan_positions(AttendPlan& a, const AttendParams& p, int row_bytes, int simd, int dtype) {
+    const size_t groups = (size_t)p.B * p.kv, tiles = (size_t)((p.N + 31) / 32) * p.per;
+    const int map = steps_of(p) * 16 * (dtype == 0 ? 144 : 64);
+    size_t bytes = resident_bytes(p.L, row_bytes, 4, map);
+    a.waves = 4;
+    if (bytes > (size_t)RESIDENT_MOST / 3 && simd > 1 && resident_bytes(p.L, row_bytes, 8, map) <= (size_t)RESIDENT_MOST) {
+        a.waves = 8;
+        bytes = resident_bytes(p.L, row_bytes, 8, map);
+    }
     a.resident = bytes <= (size_t)RESIDENT_MOST;
-    a.waves = a.resident && eight_waves && bytes > (size_t)RESIDENT_MOST / 3 ? 8 : 4;
-    a.lds = (int)bytes;
     if (!a.resident) { a.workers = (int)((tiles + 3) / 4); return; }
-    size_t fit = RESIDENT_MOST / bytes;                              // workgroups on a CU by LDS, and by registers
-    const size_t registers = (size_t)waves(dtype == 0, steps_of(p), a.wide ? 2 : 1) * 4 / a.waves;
-    if (fit > registers) fit = registers < 1 ? 1 : registers;
+    a.lds = (int)bytes;
+    size_t fit = RESIDENT_MOST / bytes;
+    if (fit > (size_t)simd * 4 / a.waves) fit = (size_t)simd * 4 / a.waves;
+    if (fit < 1) fit = 1;
     const size_t share = (256 * fit + groups - 1) / groups, turns = (tiles + share * a.waves - 1) / (share * a.waves);
     a.workers = (int)((tiles + turns * a.waves - 1) / (turns * a.waves));
 }
@@ -36,7 +39,7 @@ AttendPlan attend_plan(const AttendParams& p, int dtype) {
     a.splits = 1;
     if ((size_t)p.B * p.heads * ((p.N + 31) / 32) >= 768) {
         const int dt = (ks + 1) / 2, across = es == 4 ? dt * 128 + 32 : (dt % 2 ? dt * 64 : dt * 64 + 64);
-        plan_positions(a, p, dtype != 0 && ks <= 6, true, ks * 16 * es + 16 + across, attend_waves, dtype);
+        plan_positions(a, p, ks * 16 * es + 16 + across, attend_waves(dtype == 0, ks), dtype);
         return a;
     }
     a.few = 1;
@@ -53,7 +56,7 @@ AttendPlan attend_plan(const AttendParams& p, int dtype) {
 AttendBackPlan attend_back_plan(const AttendParams& p, int dtype) {
     AttendBackPlan a = {};
     const int ks = steps_of(p);
-    plan_positions(a.q, p, dtype != 0 && ks <= 4, dtype != 0 || ks < 7, 2 * (ks * 16 * (dtype == 0 ? 4 : 2) + 16), attend_grad_waves, dtype);
+    plan_positions(a.q, p, 2 * (ks * 16 * (dtype == 0 ? 4 : 2) + 16), attend_grad_waves(dtype == 0, ks), dtype);
     // waves along the tokens: as few idle ones as may be, a stage's way into LDS counted like one more
     size_t least = ~(size_t)0;
     for (int w = dtype == 0 && ks >= 7 ? 4 : 1; w <= 4; w *= 2) {

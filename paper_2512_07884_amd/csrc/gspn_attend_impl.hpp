@@ -75,55 +75,78 @@ template <typename T> __device__ __forceinline__ MatFrag<T> position_channels(co
     }
     return f;
 }
-// ... of two neighbouring positions with requests for both (16-bit types)
-template <typename T> __device__ __forceinline__ void position_pair_channels(const T* row, size_t N, uint32_t at, bool have, MatFrag<T>& a, MatFrag<T>& b) {
-    typedef uint32_t any4 __attribute__((aligned(2)));
-    uint32_t w[8];
+
+// 32 neighbouring positions of a head's plane [D][N], which a wave brings in requests of 16 bytes along the rows, turns in LDS of its own (`buf`, BYTES of it) and
+// gets back as operands with a lane per position; and results on the same way back.  (Two-byte requests per lane and channel: 77 tokens on
+// two 128x128 latents 48 us, the gradient of q over 300 tokens on two 64x64 maps 70.)  fp32: rows of 144 bytes, so that the two halves of
+// a wave, eight rows apart, meet other banks.
+template <typename T, int KS> struct MapTile {
+    static constexpr int E = 16 / (int)sizeof(T), PIECES = 32 / E, ROW = sizeof(T) == 4 ? 144 : 64, BYTES = KS * 16 * ROW;
+    static constexpr int COUNT = KS * 16 * PIECES / 64;
+    u32x4 r[COUNT];
+
+    // the first position of tile i: a last tile that is not whole begins earlier (the same bits twice)
+    static __device__ __forceinline__ int begin(int i, int N) { return N >= 32 ? min(i * 32, N - 32) : 0; }
+    __device__ __forceinline__ void fetch(const T* plane, int D, int N, int n0, int lane) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = have ? *(const any4*)((const uint16_t*)(row + i * N) + at) : 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        a.w[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100u);
-        b.w[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
-    }
-}
-// PT neighbouring positions n, n + 1 of a head's plane [D][N] as operands of all steps.  inside: (uniform) all positions of the wave exist; else those past
-// the end are read as the last one.
-template <typename T, int KS, int PT> __device__ __forceinline__ void load_positions(MatFrag<T> (&f)[PT][KS], const T* plane, int D, int N, int n, bool inside, int half) {
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        const bool have = 16 * s + 8 * half < D;
-        const T* row = plane + (size_t)(16 * s) * N;
-        const uint32_t up = 8u * half * N;
-        if constexpr (PT == 2) {
-            if (inside) { position_pair_channels<T>(row, N, up + n, have, f[0][s], f[1][s]); continue; }
-        }
-#pragma unroll
-        for (int t = 0; t < PT; ++t) f[t][s] = position_channels<T>(row, N, up + min(n + t, N - 1), have);
-    }
-}
-// ... and back: acc[t][i][r] * factor[t] to the channels of positions n, n + 1
-template <typename T, int DT, int PT> __device__ __forceinline__ void store_positions(const f32x16 (&acc)[PT][DT], const float (&factor)[PT], T* plane, int D, int N, int n, bool inside, int half) {
-    typedef uint32_t any4 __attribute__((aligned(2)));
-#pragma unroll
-    for (int i = 0; i < DT; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            T* row = plane + (size_t)(i * 32 + acc_row(r, 0)) * N;
-            const uint32_t up = 4u * half * N;
-            if (i * 32 + acc_row(r, half) < D) {
-                if constexpr (PT == 2 && sizeof(T) == 2) {
-                    if (inside) {
-                        *(any4*)((uint16_t*)row + up + n) = pack_word<T>(acc[0][i][r] * factor[0], acc[1][i][r] * factor[1]);
-                        continue;
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < PT; ++t)
-                    if (n + t < N) stf(row + up + n + t, acc[t][i][r] * factor[t]);
+        for (int i = 0; i < COUNT; ++i) {
+            const int c = lane + 64 * i, d = c / PIECES, n = n0 + c % PIECES * E;
+            const T* row = plane + (size_t)d * N;
+            r[i] = u32x4{0, 0, 0, 0};
+            if (d < D) {
+                if (N >= 32) r[i] = rg_load(row + n);
+                else r[i] = row_chunk(row, n, N);
             }
         }
-}
+    }
+    __device__ __forceinline__ void put(char* buf, int lane) const {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int c = lane + 64 * i;
+            *(u32x4*)(buf + c / PIECES * ROW + c % PIECES * 16) = r[i];
+        }
+    }
+    static __device__ __forceinline__ void operands(const char* buf, MatFrag<T> (&f)[KS], int lane) {
+        const int half = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[s].v[i] = *(const float*)(buf + (16 * s + 8 * half + i) * ROW + (lane & 31) * 4);
+            } else {
+                const int j = lane & 15;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x2 v = lds_turned(buf + (16 * s + 8 * half + 4 * i + (j >> 2)) * ROW + (lane & 16) * 2 + (j & 3) * 8);
+                    f[s].w[2 * i] = v.x; f[s].w[2 * i + 1] = v.y;
+                }
+            }
+        }
+    }
+    template <int DT> static __device__ __forceinline__ void store(char* buf, const f32x16 (&acc)[DT], float factor, T* plane, int D, int N, int n0, int lane) {
+        const int half = lane >> 5;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int d = i * 32 + acc_row(k, half);
+                if (i * 32 + 24 < KS * 16 || d < KS * 16) stf((T*)(buf + d * ROW) + (lane & 31), acc[i][k] * factor);
+            }
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int c = lane + 64 * i, d = c / PIECES, n = n0 + c % PIECES * E;
+            const u32x4 v = *(const u32x4*)(buf + d * ROW + c % PIECES * 16);
+            T* row = plane + (size_t)d * N;
+            if (d < D) {
+                if (N >= 32) rg_store(row + n, v);
+                else
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (n + e < N) rg_store_bits(row + n + e, rg_bits<T>(v, e));
+            }
+        }
+    }
+};
 template <typename T> __device__ __forceinline__ float frag_value(const MatFrag<T>& f, int i) {
     if constexpr (sizeof(T) == 4) return f.v[i];
     else return rg_elem<T>(f.w, i);
@@ -202,158 +225,162 @@ __device__ __forceinline__ void start_scores(f32x16& s, uint32_t word, int half)
     for (int r = 0; r < 16; ++r) s[r] = (w >> (8 * (r >> 2) + (r & 3))) & 1 ? 0.f : -__builtin_huge_valf();
 }
 
-// The running state of the wave's 32 * PT positions: output, maximum (in powers of two) and the lane's half of the sum
-template <int DT, int PT> struct AttendState {
-    f32x16 o[PT][DT];
-    float top[PT], sum[PT];
+// The running state of the wave's 32 positions: output, maximum (in powers of two) and the lane's half of the sum
+template <int DT> struct AttendState {
+    f32x16 o[DT];
+    float top, sum;
     __device__ __forceinline__ void start() {
+        top = -__builtin_huge_valf(); sum = 0.f;
 #pragma unroll
-        for (int t = 0; t < PT; ++t) {
-            top[t] = -__builtin_huge_valf(); sum[t] = 0.f;
-#pragma unroll
-            for (int i = 0; i < DT; ++i) mat_zero(o[t][i]);
-        }
+        for (int i = 0; i < DT; ++i) mat_zero(o[i]);
     }
 };
 // 32 tokens in LDS
-template <typename T, int KS, int PT>
-__device__ __forceinline__ void attend_tokens(const char* kt, const char* vt, uint32_t word, const MatFrag<T> (&q)[PT][KS], AttendState<(KS + 1) / 2, PT>& a, float c2, int lane) {
+template <typename T, int KS>
+__device__ __forceinline__ void attend_tokens(const char* kt, const char* vt, uint32_t word, const MatFrag<T> (&q)[KS], AttendState<(KS + 1) / 2>& a, float c2, int lane) {
     constexpr int DT = (KS + 1) / 2;
     const int half = lane >> 5;
-    f32x16 s[PT];
+    f32x16 s;
+    start_scores(s, word, half);
 #pragma unroll
-    for (int t = 0; t < PT; ++t) start_scores(s[t], word, half);
+    for (int i = 0; i < KS; ++i) mat_mul<T>(s, token_rows<T, KS>(kt, lane & 31, i, half), q[i]);
+    float m = s[0];
 #pragma unroll
-    for (int i = 0; i < KS; ++i) {
-        const MatFrag<T> k = token_rows<T, KS>(kt, lane & 31, i, half);
+    for (int r = 1; r < 16; ++r) m = fmaxf(m, s[r]);
+    m = other_half_max(m) * c2;
+    // The maximum is a reference that keeps the powers in range: it is moved only where it has grown by more than 2^8
+    if (__ballot(m > a.top + 8.f)) {
+        const float next = fmaxf(a.top, m), shrink = next == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(a.top - next);
+        a.top = next;
+        a.sum *= shrink;
 #pragma unroll
-        for (int t = 0; t < PT; ++t) mat_mul<T>(s[t], k, q[t][i]);
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) a.o[i][r] *= shrink;
     }
+    const float ref = a.top == -__builtin_huge_valf() ? 0.f : a.top;
+    float e[16];
 #pragma unroll
-    for (int t = 0; t < PT; ++t) {
-        float m = s[t][0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) m = fmaxf(m, s[t][r]);
-        m = other_half_max(m) * c2;
-        // The maximum is a reference that keeps the powers in range: it is moved only where it has grown by more than 2^8
-        if (__ballot(m > a.top[t] + 8.f)) {
-            const float next = fmaxf(a.top[t], m), shrink = next == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(a.top[t] - next);
-            a.top[t] = next;
-            a.sum[t] *= shrink;
-#pragma unroll
-            for (int i = 0; i < DT; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) a.o[t][i][r] *= shrink;
-        }
-        const float ref = a.top[t] == -__builtin_huge_valf() ? 0.f : a.top[t];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) { s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c2, -ref)); a.sum[t] += s[t][r]; }
-    }
+    for (int r = 0; r < 16; ++r) { e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -ref)); a.sum += e[r]; }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        MatFrag<T> w[PT];
+        const MatFrag<T> w = mat_from_acc<T>(e + 8 * j);
 #pragma unroll
-        for (int t = 0; t < PT; ++t) {
-            float e[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) e[r] = s[t][8 * j + r];
-            w[t] = mat_from_acc<T>(e);
-        }
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            const MatFrag<T> v = token_columns<T, across_pitch<T, KS>()>(vt, i, j, lane);
-#pragma unroll
-            for (int t = 0; t < PT; ++t) mat_mul<T>(a.o[t][i], v, w[t]);
-        }
+        for (int i = 0; i < DT; ++i) mat_mul<T>(a.o[i], token_columns<T, across_pitch<T, KS>()>(vt, i, j, lane), w);
     }
 }
 __device__ __forceinline__ float attend_share(float l) { return l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l); }          // (no token: 0; NaN stays NaN)
 
-// Many positions.  A wave holds 32 * PT neighbouring positions of a head (lane and lane + 32: the same ones, other channels); PT = 2 in 16 bits reads and
-// writes the maps in words of two.
-// RESIDENT: the head's tokens stay in LDS, all of them, and each wave walks over tiles of positions without meeting the others again; 77
-// tokens of 64 channels are 32 KB.  Else stages of 64 tokens, two of them in LDS, the one after them on its way in registers, and a tile per wave.
-template <typename T, int KS, int PT, int WAVES, bool RESIDENT> struct AttendShape {
+// Many positions.  A wave holds 32 neighbouring positions of a head (lane and lane + 32: the same one, other channels).
+// RESIDENT: the head's tokens stay in LDS, all of them, and each wave walks over tiles of positions without meeting the others again, the next tile on its
+// way while it works; 77 tokens of 64 channels are 32 KB.  Else stages of 64 tokens, two of them in LDS, the one after them on its way in
+// registers, and a tile per wave.
+template <typename T, int KS> struct AttendShape {
     static constexpr int TB = 64;
-    static constexpr int K_ROW = along_pitch<T, KS>(), V_ROW = across_pitch<T, KS>(), STAGE = TB * (K_ROW + V_ROW);
-    static constexpr int BUFFERS = 2 * STAGE <= 160 * 1024 ? 2 : 1;
-    static constexpr int LDS = BUFFERS * STAGE;                      // (RESIDENT: resident_bytes)
+    static constexpr int K_ROW = along_pitch<T, KS>(), V_ROW = across_pitch<T, KS>(), STAGE = TB * (K_ROW + V_ROW), MAP = MapTile<T, KS>::BYTES;
+    static constexpr int BUFFERS = 2 * STAGE + 4 * MAP <= 160 * 1024 ? 2 : 1;
+    static constexpr int LDS = BUFFERS * STAGE + 4 * MAP;            // (RESIDENT: resident_bytes)
 };
 constexpr int RESIDENT_MOST = 160 * 1024;
 // Waves per SIMD that the kernels' registers leave room for, by which a call's workgroups are counted too.  (From two on a wave has 256 registers
 // of one file, none in the accumulation file that takes a move per value read.)
-constexpr int attend_waves(bool f32, int ks, int pt) { return f32 ? (ks <= 4 ? 4 : ks <= 6 ? 3 : 2) : pt == 1 ? (ks <= 6 ? 4 : 3) : (ks <= 2 ? 4 : ks <= 4 ? 3 : 2); }
-constexpr int attend_grad_waves(bool f32, int ks, int pt) {
-    return f32 ? (ks <= 2 ? 4 : ks <= 4 ? 3 : ks <= 7 ? 2 : 1) : pt == 1 ? (ks <= 3 ? 4 : ks <= 6 ? 3 : 2) : (ks <= 2 ? 3 : 2);
-}
+constexpr int attend_waves(bool f32, int ks) { return f32 ? (ks <= 2 ? 4 : ks <= 3 ? 3 : 2) : (ks <= 4 ? 4 : ks <= 6 ? 3 : 2); }
+constexpr int attend_grad_waves(bool f32, int ks) { return f32 ? (ks <= 2 ? 3 : ks <= 5 ? 2 : 1) : (ks <= 2 ? 4 : 2); }
+// ... with the next tile of the maps in registers beside them; wide heads bring a tile when it is wanted, one map after the other
+constexpr bool attend_ahead(bool f32, int ks) { return !f32 || ks <= 6; }
+constexpr bool attend_grad_ahead(bool f32, int ks) { return f32 ? ks <= 3 : ks <= 6; }
 inline int resident_rows(int L) { return (L + 31) & ~31; }
-inline size_t resident_bytes(int L, int row) { return (size_t)resident_rows(L) * row + (size_t)(resident_rows(L) / 32 + 2) * 4 + 8; }
+// rows of the tokens, the words, a tile of the map for each wave
+inline size_t resident_bytes(int L, int row, int waves, int map) {
+    return (size_t)resident_rows(L) * row + (((size_t)(resident_rows(L) / 32 + 2) * 4 + 15) & ~(size_t)15) + (size_t)waves * map;
+}
+__device__ __forceinline__ char* resident_map(char* lds, int rows, int row, int wave, int map) { return lds + rows * row + (((rows / 32 + 2) * 4 + 15) & ~15) + wave * map; }
 
-template <typename T, int KS, int PT, int WAVES, bool RESIDENT>
-__global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_waves(sizeof(T) == 4, KS, PT) : ((sizeof(T) == 2 ? PT == 1 || KS <= 4 : KS <= 6) ? 2 : 1)) attend_kernel(const AttendParams p) {
-    using S = AttendShape<T, KS, PT, WAVES, RESIDENT>;
+template <typename T, int KS, int WAVES, bool RESIDENT>
+__global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_waves(sizeof(T) == 4, KS) : (sizeof(T) == 2 || KS <= 5 ? 2 : 1)) attend_kernel(const AttendParams p) {
+    using S = AttendShape<T, KS>;
+    using Map = MapTile<T, KS>;
     constexpr int DT = (KS + 1) / 2;
     static_assert(RESIDENT || WAVES == 4, "stages go through 256 threads");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int per_head = (p.N + 32 * PT - 1) / (32 * PT), tiles = per_head * p.per;
+    const int per_head = (p.N + 31) / 32, tiles = per_head * p.per;
     const unsigned item = xcd_contiguous_item(blockIdx.x, gridDim.x);
     const int group = item / p.workers, worker = item - group * p.workers, head = group % p.kv, b = group / p.kv;
     const float c2 = p.scale * LOG2E;
 
-    auto positions = [&](int tile, auto&& walk) {
-        const int g = tile / per_head, n = (tile - g * per_head) * 32 * PT + (lane & 31) * PT;
-        const bool inside = (tile - g * per_head + 1) * 32 * PT <= p.N;
-        const size_t plane = (size_t)b * p.heads + head * p.per + g;
-        MatFrag<T> q[PT][KS];
-        load_positions<T, KS, PT>(q, (const T*)p.q + plane * p.D * p.N, p.D, p.N, n, inside, half);
-        AttendState<DT, PT> a;
-        a.start();
-        walk(q, a);
-        float share[PT];
-#pragma unroll
-        for (int t = 0; t < PT; ++t) {
-            const float l = other_half_sum(a.sum[t]);
-            share[t] = attend_share(l);
-            if (p.lse && half == 0 && n + t < p.N) p.lse[plane * p.N + n + t] = (a.top[t] + __builtin_amdgcn_logf(l)) * LN2;
-        }
-        store_positions<T, DT, PT>(a.o, share, (T*)p.out + plane * p.D * p.N, p.D, p.N, n, inside, half);
+    auto place = [&](int tile, size_t& plane, int& n0) {
+        const int g = tile / per_head;
+        plane = (size_t)b * p.heads + head * p.per + g;
+        n0 = Map::begin(tile - g * per_head, p.N);
     };
-
+    auto finish = [&](const AttendState<DT>& a, size_t plane, int n0, char* buf) {
+        const float l = other_half_sum(a.sum);
+        if (p.lse && half == 0 && n0 + lane < p.N) p.lse[plane * p.N + n0 + lane] = (a.top + __builtin_amdgcn_logf(l)) * LN2;
+        Map::store(buf, a.o, attend_share(l), (T*)p.out + plane * p.D * p.N, p.D, p.N, n0, lane);
+    };
+    Map map;
+    size_t plane;
+    int n0;
     if constexpr (RESIDENT) {
         const int rows = (p.L + 31) & ~31;
         char* const vt = lds + rows * S::K_ROW;
         uint32_t* const words = (uint32_t*)(vt + rows * S::V_ROW);
+        char* const buf = resident_map(lds, rows, S::K_ROW + S::V_ROW, wave, S::MAP);
+        constexpr bool AHEAD = attend_ahead(sizeof(T) == 4, KS);
+        int tile = worker * WAVES + wave;
+        auto bring = [&] {
+            place(tile, plane, n0);
+            map.fetch((const T*)p.q + plane * p.D * p.N, p.D, p.N, n0, lane);
+        };
+        if (AHEAD && tile < tiles) bring();
         all_tokens<T, KS, 64 * WAVES>(p, b, head, rows, lds, S::K_ROW, vt, S::V_ROW, words, tid);
         __syncthreads();
-        for (int tile = worker * WAVES + wave; tile < tiles; tile += p.workers * WAVES)
-            positions(tile, [&](const auto& q, auto& a) {
-                for (int i = 0; i < rows / 32; ++i) {
-                    const uint32_t word = __builtin_amdgcn_readfirstlane(words[i]);
-                    if (word) attend_tokens<T, KS, PT>(lds + i * 32 * S::K_ROW, vt + i * 32 * S::V_ROW, word, q, a, c2, lane);
-                }
-            });
-    } else {
-        const int stages = (p.L + S::TB - 1) / S::TB;
-        positions(min(worker * WAVES + wave, tiles - 1), [&](const auto& q, auto& a) {       // (waves past the end: the last tile again, the same bits)
-            TokenStage<T, KS, S::TB> next;
-            next.fetch(p, b, head, 0, tid);
-            for (int st = 0; st < stages; ++st) {
-                char* const kt = lds + (S::BUFFERS == 2 ? st & 1 : 0) * S::STAGE;
-                char* const vt = kt + S::TB * S::K_ROW;
-                if (S::BUFFERS == 1 && st) lds_barrier();            // (the stage before has been read)
-                next.put(kt, S::K_ROW, vt, S::V_ROW, tid);
-                const uint64_t in = next.bits(0);
-                if (st + 1 < stages) next.fetch(p, b, head, (st + 1) * S::TB, tid);
-                lds_barrier();
-#pragma unroll
-                for (int i = 0; i < S::TB / 32; ++i) {
-                    const uint32_t word = (uint32_t)(in >> (32 * i));
-                    if (word) attend_tokens<T, KS, PT>(kt + 32 * i * S::K_ROW, vt + 32 * i * S::V_ROW, word, q, a, c2, lane);
-                }
+        while (tile < tiles) {
+            if (!AHEAD) bring();
+            const size_t at = plane;
+            const int n = n0;
+            MatFrag<T> q[KS];
+            map.put(buf, lane);
+            Map::operands(buf, q, lane);
+            tile += p.workers * WAVES;
+            if (AHEAD && tile < tiles) bring();
+            AttendState<DT> a;
+            a.start();
+            for (int i = 0; i < rows / 32; ++i) {
+                const uint32_t word = __builtin_amdgcn_readfirstlane(words[i]);
+                if (word) attend_tokens<T, KS>(lds + i * 32 * S::K_ROW, vt + i * 32 * S::V_ROW, word, q, a, c2, lane);
             }
-        });
+            finish(a, at, n, buf);
+        }
+    } else {
+        char* const buf = lds + S::BUFFERS * S::STAGE + wave * S::MAP;
+        const int stages = (p.L + S::TB - 1) / S::TB;
+        place(min(worker * WAVES + wave, tiles - 1), plane, n0);     // (waves past the end: the last tile again, the same bits)
+        map.fetch((const T*)p.q + plane * p.D * p.N, p.D, p.N, n0, lane);
+        TokenStage<T, KS, S::TB> next;
+        next.fetch(p, b, head, 0, tid);
+        MatFrag<T> q[KS];
+        map.put(buf, lane);
+        Map::operands(buf, q, lane);
+        AttendState<DT> a;
+        a.start();
+        for (int st = 0; st < stages; ++st) {
+            char* const kt = lds + (S::BUFFERS == 2 ? st & 1 : 0) * S::STAGE;
+            char* const vt = kt + S::TB * S::K_ROW;
+            if (S::BUFFERS == 1 && st) lds_barrier();                // (the stage before has been read)
+            next.put(kt, S::K_ROW, vt, S::V_ROW, tid);
+            const uint64_t in = next.bits(0);
+            if (st + 1 < stages) next.fetch(p, b, head, (st + 1) * S::TB, tid);
+            lds_barrier();
+#pragma unroll
+            for (int i = 0; i < S::TB / 32; ++i) {
+                const uint32_t word = (uint32_t)(in >> (32 * i));
+                if (word) attend_tokens<T, KS>(kt + 32 * i * S::K_ROW, vt + 32 * i * S::V_ROW, word, q, a, c2, lane);
+            }
+        }
+        finish(a, plane, n0, buf);
     }
 }
 
@@ -389,12 +416,12 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS <= 5 : KS <= 4) ? 2 
     };
     const float c2 = p.scale * LOG2E;
 
-    MatFrag<T> q[1][KS];
+    MatFrag<T> q[KS];
     const uint32_t at = offset(min(tile * 32 + (lane & 31), columns - 1));
 #pragma unroll
     for (int s = 0; s < KS; ++s)
-        q[0][s] = position_channels<T>((const T*)p.q + plane0 * p.D * p.N + (size_t)(16 * s) * p.N, p.N, at + 8u * half * p.N, 16 * s + 8 * half < p.D);
-    AttendState<DT, 1> a;
+        q[s] = position_channels<T>((const T*)p.q + plane0 * p.D * p.N + (size_t)(16 * s) * p.N, p.N, at + 8u * half * p.N, 16 * s + 8 * half < p.D);
+    AttendState<DT> a;
     a.start();
     if (first < last) {
         TokenStage<T, KS, TB> next;
@@ -409,10 +436,10 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS <= 5 : KS <= 4) ? 2 
             if (S::AHEAD && st + 1 < last) next.fetch(p, b, head, (st + 1) * TB, tid);
             lds_barrier();
             const uint32_t word = (uint32_t)(in >> (wave & 1) * 32);
-            if (word) attend_tokens<T, KS, 1>(kt + wave * 32 * S::K_ROW, vt + wave * 32 * S::V_ROW, word, q, a, c2, lane);
+            if (word) attend_tokens<T, KS>(kt + wave * 32 * S::K_ROW, vt + wave * 32 * S::V_ROW, word, q, a, c2, lane);
         }
     }
-    a.sum[0] = other_half_sum(a.sum[0]);
+    a.sum = other_half_sum(a.sum);
 
     // the four waves' states meet in LDS: [wave][channel][column], then maximum and sum
     float* const join = (float*)lds;
@@ -421,8 +448,8 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS <= 5 : KS <= 4) ? 2 
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) join[(wave * DT * 32 + i * 32 + acc_row(r, half)) * 32 + (lane & 31)] = a.o[0][i][r];
-    if (half == 0) { tops[wave * 32 + lane] = a.top[0]; tops[128 + wave * 32 + lane] = a.sum[0]; }
+        for (int r = 0; r < 16; ++r) join[(wave * DT * 32 + i * 32 + acc_row(r, half)) * 32 + (lane & 31)] = a.o[i][r];
+    if (half == 0) { tops[wave * 32 + lane] = a.top; tops[128 + wave * 32 + lane] = a.sum; }
     lds_barrier();
     const int n = tid & 31, column = tile * 32 + n;                 // a thread finishes every eighth channel of a column
     float m = tops[n], f[4], l = 0.f;
@@ -508,158 +535,160 @@ template <typename T> __global__ void __launch_bounds__(256) attend_join_kernel(
 // gq, and delta for the launch after it; positions and tokens as in attend_kernel.  Up to 64 tokens delta is the sum over the tokens, in a pass of its own
 // over what LDS holds; else the product of gout and out, which the rounding of out puts off by e: since the weights of a position add up to 1, the sum
 // of its ds is then -e, and the second launch is given delta without it.
-template <typename T, int KS, int PT, int WAVES, bool RESIDENT> struct AttendGradShape {
-    static constexpr int TB = 64, ROW = along_pitch<T, KS>(), STAGE = TB * 2 * ROW;
-    static constexpr int BUFFERS = 2 * STAGE <= 160 * 1024 ? 2 : 1;
-    static constexpr int LDS = BUFFERS * STAGE;                      // (RESIDENT: resident_bytes)
+template <typename T, int KS> struct AttendGradShape {
+    static constexpr int TB = 64, ROW = along_pitch<T, KS>(), STAGE = TB * 2 * ROW, MAP = MapTile<T, KS>::BYTES;
+    static constexpr int BUFFERS = 2 * STAGE + 4 * MAP <= 160 * 1024 ? 2 : 1;
+    static constexpr int LDS = BUFFERS * STAGE + 4 * MAP;            // (RESIDENT: resident_bytes)
 };
 // weights of 32 tokens, and the products of gout with their values
-template <typename T, int KS, int PT>
-__device__ __forceinline__ void attend_weights(const char* kt, const char* vt, uint32_t word, const MatFrag<T> (&q)[PT][KS], const MatFrag<T> (&go)[PT][KS],
-                                               const float (&ref)[PT], float c2, f32x16 (&e)[PT], f32x16 (&dp)[PT], int lane) {
+template <typename T, int KS>
+__device__ __forceinline__ void attend_weights(const char* kt, const char* vt, uint32_t word, const MatFrag<T> (&q)[KS], const MatFrag<T> (&go)[KS],
+                                               float ref, float c2, f32x16& e, f32x16& dp, int lane) {
     const int half = lane >> 5;
-#pragma unroll
-    for (int t = 0; t < PT; ++t) { start_scores(e[t], word, half); mat_zero(dp[t]); }
+    start_scores(e, word, half);
+    mat_zero(dp);
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
-        const MatFrag<T> k = token_rows<T, KS>(kt, lane & 31, i, half), v = token_rows<T, KS>(vt, lane & 31, i, half);
-#pragma unroll
-        for (int t = 0; t < PT; ++t) { mat_mul<T>(e[t], k, q[t][i]); mat_mul<T>(dp[t], v, go[t][i]); }
+        mat_mul<T>(e, token_rows<T, KS>(kt, lane & 31, i, half), q[i]);
+        mat_mul<T>(dp, token_rows<T, KS>(vt, lane & 31, i, half), go[i]);
     }
 #pragma unroll
-    for (int t = 0; t < PT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) e[t][r] = __builtin_amdgcn_exp2f(fmaf(e[t][r], c2, -ref[t]));
+    for (int r = 0; r < 16; ++r) e[r] = __builtin_amdgcn_exp2f(fmaf(e[r], c2, -ref));
 }
-template <typename T, int KS, int PT, int WAVES, bool RESIDENT>
-__global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_grad_waves(sizeof(T) == 4, KS, PT) : ((sizeof(T) == 2 ? KS < 8 && (PT == 1 || KS < 4) : KS <= 4) ? 2 : 1)) attend_grad_q_kernel(const AttendParams p) {
-    using S = AttendGradShape<T, KS, PT, WAVES, RESIDENT>;
+template <typename T, int KS, int WAVES, bool RESIDENT>
+__global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_grad_waves(sizeof(T) == 4, KS) : (sizeof(T) == 2 ? KS < 7 : KS <= 3) ? 2 : 1) attend_grad_q_kernel(const AttendParams p) {
+    using S = AttendGradShape<T, KS>;
+    using Map = MapTile<T, KS>;
     constexpr int DT = (KS + 1) / 2;
     static_assert(RESIDENT || WAVES == 4, "stages go through 256 threads");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int per_head = (p.N + 32 * PT - 1) / (32 * PT), tiles = per_head * p.per;
+    const int per_head = (p.N + 31) / 32, tiles = per_head * p.per;
     const unsigned item = xcd_contiguous_item(blockIdx.x, gridDim.x);
     const int group = item / p.workers, worker = item - group * p.workers, head = group % p.kv, b = group / p.kv;
     const float c2 = p.scale * LOG2E;
     const bool few = p.L <= 64;
 
-    auto positions = [&](int tile, auto&& walk) {
-        const int g = tile / per_head, n = (tile - g * per_head) * 32 * PT + (lane & 31) * PT;
-        const bool inside = (tile - g * per_head + 1) * 32 * PT <= p.N;
-        const size_t plane = (size_t)b * p.heads + head * p.per + g, at = plane * p.D * p.N;
-        MatFrag<T> q[PT][KS], go[PT][KS];
-        load_positions<T, KS, PT>(q, (const T*)p.q + at, p.D, p.N, n, inside, half);
-        load_positions<T, KS, PT>(go, (const T*)p.gout + at, p.D, p.N, n, inside, half);
-        float delta[PT], ref[PT], off[PT], scale[PT];
-#pragma unroll
-        for (int t = 0; t < PT; ++t) {
-            const float lse = p.lse[plane * p.N + min(n + t, p.N - 1)];
-            ref[t] = lse == -__builtin_huge_valf() ? __builtin_huge_valf() : lse * LOG2E;        // (no token: all weights 0)
-            delta[t] = off[t] = 0.f;
-            scale[t] = p.scale;
+    constexpr bool AHEAD = attend_grad_ahead(sizeof(T) == 4, KS);
+    Map maps[AHEAD ? 3 : 1];
+    Map &mq = maps[0], &mg = maps[AHEAD ? 1 : 0], &mo = maps[AHEAD ? 2 : 0];
+    float lse;
+    size_t plane;
+    int n0;
+    auto bring = [&](Map& m, const void* from) { m.fetch((const T*)from + plane * p.D * p.N, p.D, p.N, n0, lane); };
+    auto fetch = [&](int tile) {
+        const int g = tile / per_head;
+        plane = (size_t)b * p.heads + head * p.per + g;
+        n0 = Map::begin(tile - g * per_head, p.N);
+        bring(mq, p.q);
+        if (AHEAD) {
+            bring(mg, p.gout);
+            if (!few) bring(mo, p.out);
         }
+        lse = p.lse[plane * p.N + min(n0 + (lane & 31), p.N - 1)];
+    };
+    MatFrag<T> q[KS], go[KS];
+    float delta, off, ref;                                           // off: the sum of ds
+    f32x16 acc[DT];
+    auto start = [&](char* buf) {
+        mq.put(buf, lane);
+        Map::operands(buf, q, lane);
+        if (!AHEAD) bring(mg, p.gout);
+        mg.put(buf, lane);
+        Map::operands(buf, go, lane);
+        delta = off = 0.f;
         if (!few) {
+            MatFrag<T> out[KS];
+            if (!AHEAD) bring(mo, p.out);
+            mo.put(buf, lane);
+            Map::operands(buf, out, lane);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                MatFrag<T> out[PT][1];
-                load_positions<T, 1, PT>(out, (const T*)p.out + at + (size_t)(16 * s) * p.N, p.D - 16 * s, p.N, n, inside, half);
+            for (int s = 0; s < KS; ++s)
 #pragma unroll
-                for (int t = 0; t < PT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) delta[t] = fmaf(frag_value<T>(go[t][s], i), frag_value<T>(out[t][0], i), delta[t]);
-            }
-#pragma unroll
-            for (int t = 0; t < PT; ++t) delta[t] = other_half_sum(delta[t]);
+                for (int i = 0; i < 8; ++i) delta = fmaf(frag_value<T>(go[s], i), frag_value<T>(out[s], i), delta);
+            delta = other_half_sum(delta);
         }
-        f32x16 acc[PT][DT];
+        ref = lse == -__builtin_huge_valf() ? __builtin_huge_valf() : lse * LOG2E;              // (no token: all weights 0)
 #pragma unroll
-        for (int t = 0; t < PT; ++t)
+        for (int i = 0; i < DT; ++i) mat_zero(acc[i]);
+    };
+    // 32 tokens: towards delta, or their share of gq
+    auto sum_delta = [&](const char* kt, const char* vt, uint32_t word) {
+        f32x16 e, dp;
+        attend_weights<T, KS>(kt, vt, word, q, go, ref, c2, e, dp, lane);
 #pragma unroll
-            for (int i = 0; i < DT; ++i) mat_zero(acc[t][i]);
-        // 32 tokens: towards delta, or their share of gq
-        auto sum_delta = [&](const char* kt, const char* vt, uint32_t word) {
-            f32x16 e[PT], dp[PT];
-            attend_weights<T, KS, PT>(kt, vt, word, q, go, ref, c2, e, dp, lane);
+        for (int r = 0; r < 16; ++r) delta = fmaf(e[r], dp[r], delta);
+    };
+    auto step = [&](const char* kt, const char* vt, uint32_t word) {
+        f32x16 e, dp;
+        attend_weights<T, KS>(kt, vt, word, q, go, ref, c2, e, dp, lane);
 #pragma unroll
-            for (int t = 0; t < PT; ++t)
+        for (int j = 0; j < 2; ++j) {
+            float x[8];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) off[t] = fmaf(e[t][r], dp[t][r], off[t]);
-        };
-        auto step = [&](const char* kt, const char* vt, uint32_t word) {
-            f32x16 e[PT], dp[PT];
-            attend_weights<T, KS, PT>(kt, vt, word, q, go, ref, c2, e, dp, lane);
-            MatFrag<T> ds[PT][2];
+            for (int r = 0; r < 8; ++r) { x[r] = e[8 * j + r] * (dp[8 * j + r] - delta); off += x[r]; }
+            const MatFrag<T> ds = mat_from_acc<T>(x);
 #pragma unroll
-            for (int t = 0; t < PT; ++t)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    float x[8];
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) { x[r] = e[t][8 * j + r] * (dp[t][8 * j + r] - delta[t]); off[t] += x[r]; }
-                    ds[t][j] = mat_from_acc<T>(x);
-                }
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    const MatFrag<T> k = token_columns<T, S::ROW>(kt, i, j, lane);
-#pragma unroll
-                    for (int t = 0; t < PT; ++t) mat_mul<T>(acc[t][i], k, ds[t][j]);
-                }
-        };
-        walk(sum_delta, [&] {
-#pragma unroll
-            for (int t = 0; t < PT; ++t) { delta[t] = other_half_sum(off[t]); off[t] = 0.f; }
-        }, step);
-#pragma unroll
-        for (int t = 0; t < PT; ++t) {
-            const float exact = delta[t] + other_half_sum(off[t]);
-            if (half == 0 && n + t < p.N) p.delta[plane * p.N + n + t] = exact;
+            for (int i = 0; i < DT; ++i) mat_mul<T>(acc[i], token_columns<T, S::ROW>(kt, i, j, lane), ds);
         }
-        if (p.gq) store_positions<T, DT, PT>(acc, scale, (T*)p.gq + at, p.D, p.N, n, inside, half);
+    };
+    auto finish = [&](size_t at, int n, char* buf) {
+        const float exact = delta + other_half_sum(off);
+        if (half == 0 && n + lane < p.N) p.delta[at * p.N + n + lane] = exact;
+        if (p.gq) Map::store(buf, acc, p.scale, (T*)p.gq + at * p.D * p.N, p.D, p.N, n, lane);
     };
 
     if constexpr (RESIDENT) {
         const int rows = (p.L + 31) & ~31;
         char* const vt = lds + rows * S::ROW;
         uint32_t* const words = (uint32_t*)(vt + rows * S::ROW);
+        char* const buf = resident_map(lds, rows, 2 * S::ROW, wave, S::MAP);
+        int tile = worker * WAVES + wave;
+        if (AHEAD && tile < tiles) fetch(tile);
         all_tokens<T, KS, 64 * WAVES>(p, b, head, rows, lds, S::ROW, vt, S::ROW, words, tid);
         __syncthreads();
-        for (int tile = worker * WAVES + wave; tile < tiles; tile += p.workers * WAVES)
-            positions(tile, [&](auto&& sum_delta, auto&& summed, auto&& step) {
-                if (few) {
-                    for (int i = 0; i < rows / 32; ++i) {
-                        const uint32_t word = __builtin_amdgcn_readfirstlane(words[i]);
-                        if (word) sum_delta(lds + i * 32 * S::ROW, vt + i * 32 * S::ROW, word);
-                    }
-                    summed();
-                }
+        while (tile < tiles) {
+            if (!AHEAD) fetch(tile);
+            const size_t at = plane;
+            const int n = n0;
+            start(buf);
+            tile += p.workers * WAVES;
+            if (AHEAD && tile < tiles) fetch(tile);
+            if (few) {
                 for (int i = 0; i < rows / 32; ++i) {
                     const uint32_t word = __builtin_amdgcn_readfirstlane(words[i]);
-                    if (word) step(lds + i * 32 * S::ROW, vt + i * 32 * S::ROW, word);
+                    if (word) sum_delta(lds + i * 32 * S::ROW, vt + i * 32 * S::ROW, word);
                 }
-            });
-    } else {
-        const int stages = (p.L + S::TB - 1) / S::TB;
-        positions(min(worker * WAVES + wave, tiles - 1), [&](auto&&, auto&&, auto&& step) {     // (waves past the end: the last tile again, the same bits)
-            TokenStage<T, KS, S::TB> next;
-            next.fetch(p, b, head, 0, tid);
-            for (int st = 0; st < stages; ++st) {
-                char* const kt = lds + (S::BUFFERS == 2 ? st & 1 : 0) * S::STAGE;
-                char* const vt = kt + S::TB * S::ROW;
-                if (S::BUFFERS == 1 && st) lds_barrier();
-                next.put(kt, S::ROW, vt, S::ROW, tid);
-                const uint64_t in = next.bits(0);
-                if (st + 1 < stages) next.fetch(p, b, head, (st + 1) * S::TB, tid);
-                lds_barrier();
-                for (int i = 0; i < S::TB / 32; ++i) {
-                    const uint32_t word = (uint32_t)(in >> (32 * i));
-                    if (word) step(kt + 32 * i * S::ROW, vt + 32 * i * S::ROW, word);
-                }
+                delta = other_half_sum(delta);
             }
-        });
+            for (int i = 0; i < rows / 32; ++i) {
+                const uint32_t word = __builtin_amdgcn_readfirstlane(words[i]);
+                if (word) step(lds + i * 32 * S::ROW, vt + i * 32 * S::ROW, word);
+            }
+            finish(at, n, buf);
+        }
+    } else {
+        char* const buf = lds + S::BUFFERS * S::STAGE + wave * S::MAP;
+        const int stages = (p.L + S::TB - 1) / S::TB;
+        fetch(min(worker * WAVES + wave, tiles - 1));                // (waves past the end: the last tile again, the same bits)
+        TokenStage<T, KS, S::TB> next;
+        next.fetch(p, b, head, 0, tid);
+        start(buf);
+        for (int st = 0; st < stages; ++st) {
+            char* const kt = lds + (S::BUFFERS == 2 ? st & 1 : 0) * S::STAGE;
+            char* const vt = kt + S::TB * S::ROW;
+            if (S::BUFFERS == 1 && st) lds_barrier();
+            next.put(kt, S::ROW, vt, S::ROW, tid);
+            const uint64_t in = next.bits(0);
+            if (st + 1 < stages) next.fetch(p, b, head, (st + 1) * S::TB, tid);
+            lds_barrier();
+            for (int i = 0; i < S::TB / 32; ++i) {
+                const uint32_t word = (uint32_t)(in >> (32 * i));
+                if (word) step(kt + 32 * i * S::ROW, vt + 32 * i * S::ROW, word);
+            }
+        }
+        finish(plane, n0, buf);
     }
 }
 
@@ -867,15 +896,11 @@ template <typename K> hipError_t attend_launch(K kernel, size_t items, int threa
     hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(threads), lds, s, p);
     return hipGetLastError();
 }
-// Positions of a wave that can be two neighbouring ones per lane: 16 bits, and heads for whose state there are registers
-template <typename T, int KS> constexpr bool attend_wide() { return sizeof(T) == 2 && KS <= 6; }
-template <typename T, int KS> constexpr bool attend_grad_wide() { return sizeof(T) == 2 && KS <= 4; }
-
-template <typename T, int KS, int PT> hipError_t launch_attend_many(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
+template <typename T, int KS> hipError_t launch_attend_many(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
     const size_t groups = (size_t)p.B * p.kv;
-    if (plan.waves == 8) return attend_launch(attend_kernel<T, KS, PT, 8, true>, groups * p.workers, 512, plan.lds, p, s);
-    if (plan.resident) return attend_launch(attend_kernel<T, KS, PT, 4, true>, groups * p.workers, 256, plan.lds, p, s);
-    return attend_launch(attend_kernel<T, KS, PT, 4, false>, groups * p.workers, 256, AttendShape<T, KS, PT, 4, false>::LDS, p, s);
+    if (plan.waves == 8) return attend_launch(attend_kernel<T, KS, 8, true>, groups * p.workers, 512, plan.lds, p, s);
+    if (plan.resident) return attend_launch(attend_kernel<T, KS, 4, true>, groups * p.workers, 256, plan.lds, p, s);
+    return attend_launch(attend_kernel<T, KS, 4, false>, groups * p.workers, 256, AttendShape<T, KS>::LDS, p, s);
 }
 template <typename T, int KS> hipError_t launch_attend_head(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
     if (plan.few) {
@@ -884,23 +909,20 @@ template <typename T, int KS> hipError_t launch_attend_head(const AttendParams& 
         if (e != hipSuccess || p.splits == 1) return e;
         return attend_launch(attend_join_kernel<T>, (size_t)p.B * p.kv * tiles * ((p.D + 7) / 8), 256, (p.splits + 8) * 32 * 4, p, s);
     }
-    if constexpr (attend_wide<T, KS>()) { if (plan.wide) return launch_attend_many<T, KS, 2>(p, plan, s); }
-    return launch_attend_many<T, KS, 1>(p, plan, s);
+    return launch_attend_many<T, KS>(p, plan, s);
 }
-template <typename T, int KS, int PT> hipError_t launch_grad_q(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
+template <typename T, int KS> hipError_t launch_grad_q(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
     const size_t groups = (size_t)p.B * p.kv;
-    if constexpr (sizeof(T) == 2 || KS < 7) {                        // (registers)
-        if (plan.waves == 8) return attend_launch(attend_grad_q_kernel<T, KS, PT, 8, true>, groups * p.workers, 512, plan.lds, p, s);
+    if constexpr (attend_grad_waves(sizeof(T) == 4, KS) > 1) {
+        if (plan.waves == 8) return attend_launch(attend_grad_q_kernel<T, KS, 8, true>, groups * p.workers, 512, plan.lds, p, s);
     }
-    if (plan.resident) return attend_launch(attend_grad_q_kernel<T, KS, PT, 4, true>, groups * p.workers, 256, plan.lds, p, s);
-    return attend_launch(attend_grad_q_kernel<T, KS, PT, 4, false>, groups * p.workers, 256, AttendGradShape<T, KS, PT, 4, false>::LDS, p, s);
+    if (plan.resident) return attend_launch(attend_grad_q_kernel<T, KS, 4, true>, groups * p.workers, 256, plan.lds, p, s);
+    return attend_launch(attend_grad_q_kernel<T, KS, 4, false>, groups * p.workers, 256, AttendGradShape<T, KS>::LDS, p, s);
 }
 template <typename T, int KS> hipError_t launch_attend_bwd_head(const AttendParams& p, const AttendBackPlan& plan, hipStream_t s) {
     AttendParams q = p;
     q.workers = plan.q.workers;
-    hipError_t e;
-    if constexpr (attend_grad_wide<T, KS>()) e = plan.q.wide ? launch_grad_q<T, KS, 2>(q, plan.q, s) : launch_grad_q<T, KS, 1>(q, plan.q, s);
-    else e = launch_grad_q<T, KS, 1>(q, plan.q, s);
+    hipError_t e = launch_grad_q<T, KS>(q, plan.q, s);
     if (e != hipSuccess || (!p.gk && !p.gv)) return e;
     const size_t items = (size_t)p.B * p.kv * p.splits * ((p.L + 32 * plan.token_waves - 1) / (32 * plan.token_waves));
     if constexpr (sizeof(T) == 2 || KS < 7) {                        // (fp32 heads of more than 96 channels: registers for four token waves alone)

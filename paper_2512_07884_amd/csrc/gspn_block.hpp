@@ -52,9 +52,9 @@ struct AttendParams {
     int splits;                      // stretches of the tokens (forward), of the positions (backward)
     int workers;                     // workgroups per head of the tokens
 };
-// How a call runs.  few: the waves of a workgroup on the tokens instead of the positions, in `splits` stretches; else: wide: 64 positions per wave instead of 32;
+// How a call runs.  few: the waves of a workgroup on the tokens instead of the positions, in `splits` stretches; else
 // resident: a head's tokens all in LDS (`lds` bytes); waves of a workgroup; workgroups per head of the tokens.
-struct AttendPlan { int few, wide, resident, waves, workers, splits, lds; size_t bytes; };
+struct AttendPlan { int few, resident, waves, workers, splits, lds; size_t bytes; };
 AttendPlan attend_plan(const AttendParams& p, int dtype);
 // backward: the launch of gq; for gk and gv waves along the tokens (4, 2 or 1; the others along the positions) and stretches of the positions
 struct AttendBackPlan { AttendPlan q; int token_waves, splits, parts; size_t delta_bytes, bytes; };
