@@ -10,11 +10,10 @@ size_t tiles_of(const ProductParams& p, bool gated, int bm, int bn, int images) 
     return (size_t)((p.M + rows - 1) / rows) * ((p.N + bn - 1) / bn) * images;
 }
 
-// Large tiles where they are one for every CU or more; smaller ones, with several waves over the contracted axis, where they are not.
-// 256 x 256 in 16 bits reads each operand half as often, but a CU holds one of those: where three quarters of what the CUs compute is wanted, or three fifths over a
-// long contraction.
+// 256 x 256 in 16 bits reads each operand half as often as 128 x 128, but a CU holds one of those: where three quarters of what the CUs compute is wanted, or
+// three fifths over a long contraction.
 bool huge_tiles(const ProductParams& p, int form, bool gated, int images, int dtype) {
-    if (dtype == 0 || p.K < 512) return false;
+    if (dtype == 0 || p.K < 256) return false;
     const bool direct = gated ? product_direct<ProductShape<bf16_t, PRODUCT_FORWARD, OUT_GATED, 2, 2, 4, 4, 1>>(p, form, 8, 2)
                               : product_direct<ProductShape<bf16_t, PRODUCT_FORWARD, OUT_PROJECT, 2, 2, 4, 4, 1>>(p, form, 8, 2);
     if (!direct) return false;
@@ -22,18 +21,33 @@ bool huge_tiles(const ProductParams& p, int form, bool gated, int images, int dt
     const double used = (double)rows * p.N * images / ((double)((tiles + 255) / 256) * 256 * 65536);
     return used >= 0.75 || (used >= 0.6 && p.K >= 2048);
 }
+// The gradient of the matrix: 64 x 64 where those, with the pixels cut into as many stretches as make two workgroups for every CU, use three quarters of them.
+// 128 x 128 and 64 x 64, each at its best number of stretches (us): bf16 512 x 512 on two 64x64 maps 27 18, 1536 x 384 on four 32x32 26 20, 2048 x 1024 on two
+// 64x64 63 55, 1152 x 1152 (not three quarters) 44 51; fp32 2048 x 256 on eight 32x32 87 77, 1152 x 144 on two 64x64 68 44.
+bool medium_gradient(const ProductParams& p) {
+    const size_t tiles = tiles_of(p, false, 64, 64, 1);
+    return p.M <= 64 || p.N <= 64 || (tiles <= 512 && 512 / tiles * tiles >= 384);
+}
+// Large tiles where there are two for every CU; flat ones where there are nearly as many of those; smaller ones, with several waves over the contracted axis,
+// where there are not.  Rows of fewer pixels than a tile has columns are requested piece by piece, so a narrower tile comes first.
+// Times (us) on 128 x 128, 32 x 128, 64 x 64, 64 x 32 tiles: bf16 1152 x 144 on two 64x64 maps 13 14 20 58, 384 x 384 on eight 28x28 13 9 11 21, 144 x 1152 on two
+// 64x64 22 12 10 20, 512 x 512 on one 33x33 15 9 8 11, 768 x 768 on 64 of 7x7 56 92 54 34; fp32 1024 x 1024 on two 64x64 135 - - -, 96 x 96 on 64 of
+// 56x56 71 51 93 196, 384 x 384 on eight 28x28 32 24 27 33, 96 x 384 on one 14x14 31 11 11 8.
 int product_tile(const ProductParams& p, int form, int outcome, int dtype) {
     const bool gated = outcome == OUT_GATED || outcome == OUT_GATED_GRAD;
-    if (form == PRODUCT_GRAD_MATRIX) return p.M <= 64 || p.N <= 64 ? TILE_MEDIUM : (huge_tiles(p, form, false, 1, dtype) ? TILE_HUGE : TILE_LARGE);
-    if (!gated && p.M <= 32 && tiles_of(p, false, 32, 128, p.images) >= 256) return TILE_FLAT;
-    if (huge_tiles(p, form, gated, p.images, dtype)) return TILE_HUGE;
-    if (tiles_of(p, gated, 128, 128, p.images) >= 256) return TILE_LARGE;
-    return tiles_of(p, gated, 64, 64, p.images) >= 256 ? TILE_MEDIUM : TILE_SMALL;
+    if (form == PRODUCT_GRAD_MATRIX) return medium_gradient(p) ? TILE_MEDIUM : (huge_tiles(p, form, false, 1, dtype) ? TILE_HUGE : TILE_LARGE);
+    if (p.N < 64) return TILE_SMALL;
+    if (p.N >= 128) {
+        if (huge_tiles(p, form, gated, p.images, dtype)) return TILE_HUGE;
+        if (tiles_of(p, gated, 128, 128, p.images) >= 512 && (dtype != 0 || p.K >= 512) && p.M > 32) return TILE_LARGE;
+        if (tiles_of(p, gated, gated ? 64 : 32, 128, p.images) >= (dtype == 0 ? 256 : 448)) return TILE_FLAT;
+    }
+    return tiles_of(p, gated, 64, 64, p.images) >= 128 ? TILE_MEDIUM : TILE_SMALL;
 }
 // a tile's side, its columns and the waves along them
 void tile_columns(int tile, int* bn, int* wn) {
-    *bn = tile == TILE_HUGE ? 256 : tile == TILE_LARGE || tile == TILE_FLAT ? 128 : (tile == TILE_MEDIUM ? 64 : 32);
-    *wn = tile == TILE_FLAT || tile == TILE_HUGE ? 4 : (tile == TILE_SMALL ? 1 : 2);
+    *bn = tile == TILE_HUGE ? 256 : (tile == TILE_MEDIUM ? 64 : (tile == TILE_SMALL ? 32 : 128));
+    *wn = tile == TILE_SMALL ? 1 : (tile == TILE_LARGE || tile == TILE_MEDIUM ? 2 : 4);
 }
 
 // Few parts: a thread adds those of four neighbouring results, in order
@@ -55,7 +69,7 @@ template <typename T> __global__ void __launch_bounds__(256) sum_few_kernel(cons
     }
     for (int e = 0; e < have; ++e) stf(out + i + e, sum[e]);
 }
-// Many parts of few results: 32 neighbouring results per workgroup, each thread every 32nd part of one, the 32 sums added in order
+// Many parts of few results (a thousand threads per 32 of them): 32 neighbouring results per workgroup, each thread every 32nd part of one, the 32 sums added in order
 template <typename T> __global__ void __launch_bounds__(1024) sum_many_kernel(const float* __restrict__ in, T* __restrict__ out, int parts, size_t n, const float* __restrict__ in2, T* __restrict__ out2) {
     if (blockIdx.y) { in = in2; out = out2; }
     __shared__ float strip[32][33];
@@ -76,7 +90,7 @@ template <typename T> __global__ void __launch_bounds__(1024) sum_many_kernel(co
 template <typename T> hipError_t sum_parts_as(const float* in, void* out_, int parts, size_t n, hipStream_t s, const float* in2, void* out2_) {
     T *const out = (T*)out_, *const out2 = (T*)out2_;
     const unsigned sums = out2 ? 2 : 1;
-    const bool many = parts > 16;
+    const bool many = parts > 16 && n <= 32768;
     const size_t blocks = many ? (n + 31) / 32 : (n + 1023) / 1024;
     if (blocks * 1024 >= ((size_t)1 << 32)) return hipErrorInvalidValue;
     if (many) hipLaunchKernelGGL(sum_many_kernel<T>, dim3((unsigned)blocks, sums), dim3(1024), 0, s, in, out, parts, n, in2, out2);
@@ -117,7 +131,8 @@ int product_splits(const ProductParams& p, int dtype) {
     const int tile = product_tile(p, PRODUCT_GRAD_MATRIX, OUT_PLAIN, dtype);
     const int side = tile == TILE_HUGE ? 256 : (tile == TILE_LARGE ? 128 : 64), stage = dtype == 0 ? 32 : 64;
     const size_t tiles = tiles_of(p, false, side, side, 1), stages = (size_t)((p.K + stage - 1) / stage) * p.images;
-    size_t n = tile == TILE_HUGE ? 256 / tiles : (512 + tiles / 2) / tiles;
+    // (a call of 64 x 64 has two of them in a stage)
+    size_t n = tile == TILE_HUGE ? 256 / tiles : (tile == TILE_LARGE ? (512 + tiles / 2) / tiles : 512 / tiles);
     if (n > stages / 6) n = stages / 6;
     return n < 1 ? 1 : (int)n;
 }

@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) product_kernel(const Produc
 }
 
 // tiles: 0: 128 x 128 (2 x 2 waves of 64 x 64); 1: 64 x 64 (two waves along the pixels, two along the stage); 2: 64 x 32 (four along the
-// stage); 3: 32 x 128 (few rows); 4: 256 x 256 (4 x 4 waves)
+// stage); 3: 32 x 128 (four waves along the pixels; gated: 64 rows of P); 4: 256 x 256 (4 x 4 waves)
 enum { TILE_LARGE = 0, TILE_MEDIUM = 1, TILE_SMALL = 2, TILE_FLAT = 3, TILE_HUGE = 4 };
 
 // Requests straight to LDS: whole rows of 16-byte pieces, and offsets of 32 bits
@@ -517,11 +517,11 @@ template <typename S> bool product_direct(const ProductParams& p, int form, int 
 template <typename T, int FORM, int OUTC, int MT, int NT, int WM, int WN, int WK, int RB = 128, int NBUF = 2, bool ONLY_DIRECT = false>
 hipError_t launch_product_tile(const ProductParams& p, hipStream_t s) {
     using S = ProductShape<T, FORM, OUTC, MT, NT, WM, WN, WK, RB, NBUF>;
-    using R = ProductShape<T, FORM, OUTC, MT, NT, WM, WN, WK>;       // through registers: two buffers of whole lines
+    using R = ProductShape<T, FORM, OUTC, MT, NT, WM, WN, WK, RB, 2>;       // through registers: two buffers
     const bool direct = product_direct<S>(p, FORM, S::E, sizeof(T));
     auto kernel = product_kernel<T, FORM, OUTC, MT, NT, WM, WN, WK, true, RB, NBUF>;
     if constexpr (ONLY_DIRECT) { if (!direct) return hipErrorInvalidValue; }         // (product_tile does not choose it then)
-    else if (!direct) kernel = product_kernel<T, FORM, OUTC, MT, NT, WM, WN, WK, false, 128, 2>;
+    else if (!direct) kernel = product_kernel<T, FORM, OUTC, MT, NT, WM, WN, WK, false, RB, 2>;
     const int lds = direct ? S::LDS : R::LDS;
     hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
