@@ -7,14 +7,14 @@ namespace {
 size_t rounded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
 int steps_of(const AttendParams& p) { return (p.D + 15) / 16; }
-// The launch over the positions, 32 per wave.  A head's tokens stay in LDS where all of them fit; four waves share up to a third of a CU's LDS, eight what is
-// more; as many workgroups per head as fill the chip (by LDS, and by `simd` waves per SIMD), each with equal shares of the head's tiles.
-void plan_positions(AttendPlan& a, const AttendParams& p, int row_bytes, int simd, int dtype) {
+// The launch over the positions, 32 per wave.  A head's tokens stay in LDS where all of them fit; four waves share up to a third of a CU's LDS, eight (where
+// there is a kernel of eight) what is more; as many workgroups per head as fill the chip (by LDS, and by `simd` waves per SIMD), each with equal shares of the head's tiles.
+void plan_positions(AttendPlan& a, const AttendParams& p, int row_bytes, int simd, bool eight, int dtype) {
     const size_t groups = (size_t)p.B * p.kv, tiles = (size_t)((p.N + 31) / 32) * p.per;
     const int map = steps_of(p) * 16 * (dtype == 0 ? 144 : 64);
     size_t bytes = resident_bytes(p.L, row_bytes, 4, map);
     a.waves = 4;
-    if (bytes > (size_t)RESIDENT_MOST / 3 && simd > 1 && resident_bytes(p.L, row_bytes, 8, map) <= (size_t)RESIDENT_MOST) {
+    if (bytes > (size_t)RESIDENT_MOST / 3 && eight && resident_bytes(p.L, row_bytes, 8, map) <= (size_t)RESIDENT_MOST) {
         a.waves = 8;
         bytes = resident_bytes(p.L, row_bytes, 8, map);
     }
@@ -39,7 +39,8 @@ AttendPlan attend_plan(const AttendParams& p, int dtype) {
     a.splits = 1;
     if ((size_t)p.B * p.heads * ((p.N + 31) / 32) >= 768) {
         const int dt = (ks + 1) / 2, across = es == 4 ? dt * 128 + 32 : (dt % 2 ? dt * 64 : dt * 64 + 64);
-        plan_positions(a, p, ks * 16 * es + 16 + across, attend_waves(dtype == 0, ks), dtype);
+        const bool both = es == 2 && p.L <= SPLIT_MOST;
+        plan_positions(a, p, ks * 16 * es + 16 + across, both ? (ks <= 4 ? 3 : 2) : attend_waves(dtype == 0, ks), !both, dtype);
         return a;
     }
     a.few = 1;
@@ -56,7 +57,7 @@ AttendPlan attend_plan(const AttendParams& p, int dtype) {
 AttendBackPlan attend_back_plan(const AttendParams& p, int dtype) {
     AttendBackPlan a = {};
     const int ks = steps_of(p);
-    plan_positions(a.q, p, 2 * (ks * 16 * (dtype == 0 ? 4 : 2) + 16), attend_grad_waves(dtype == 0, ks), dtype);
+    plan_positions(a.q, p, 2 * (ks * 16 * (dtype == 0 ? 4 : 2) + 16), attend_grad_waves(dtype == 0, ks), attend_grad_waves(dtype == 0, ks) > 1, dtype);
     // waves along the tokens: as few idle ones as may be, a stage's way into LDS counted like one more
     size_t least = ~(size_t)0;
     for (int w = dtype == 0 && ks >= 7 ? 4 : 1; w <= 4; w *= 2) {

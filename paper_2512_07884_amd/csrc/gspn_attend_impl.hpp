@@ -15,6 +15,11 @@
 
 namespace gspn {
 
+// 16 bits.  The weights are rounded for their products; of many tokens those errors come out as that of one more rounding of the result.  Of few tokens, with
+// weights about a half, they are larger (1.6 times a rounding's error in all), and there is time, as the maps bound such calls: up to this many
+// tokens the products take what the rounding left as well.  gq, which also has the rounding of out in it (delta), always takes it of ds: its error
+// over 300 tokens was 1.5 times a rounding's, for 5 us of 124 of that step.
+constexpr int SPLIT_MOST = 64;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // the value of the lane 32 away as well: both halves of the wave
@@ -236,7 +241,7 @@ template <int DT> struct AttendState {
     }
 };
 // 32 tokens in LDS
-template <typename T, int KS>
+template <typename T, int KS, bool BOTH>
 __device__ __forceinline__ void attend_tokens(const char* kt, const char* vt, uint32_t word, const MatFrag<T> (&q)[KS], AttendState<(KS + 1) / 2>& a, float c2, int lane) {
     constexpr int DT = (KS + 1) / 2;
     const int half = lane >> 5;
@@ -264,9 +269,20 @@ __device__ __forceinline__ void attend_tokens(const char* kt, const char* vt, ui
     for (int r = 0; r < 16; ++r) { e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -ref)); a.sum += e[r]; }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const MatFrag<T> w = mat_from_acc<T>(e + 8 * j);
+        MatFrag<T> w, rest;
+        if constexpr (BOTH) {
+            mat_split<T>(e + 8 * j, w, rest);
 #pragma unroll
-        for (int i = 0; i < DT; ++i) mat_mul<T>(a.o[i], token_columns<T, across_pitch<T, KS>()>(vt, i, j, lane), w);
+            for (int i = 0; i < DT; ++i) {
+                const MatFrag<T> v = token_columns<T, across_pitch<T, KS>()>(vt, i, j, lane);
+                mat_mul<T>(a.o[i], v, w);
+                mat_mul<T>(a.o[i], v, rest);
+            }
+        } else {
+            w = mat_from_acc<T>(e + 8 * j);
+#pragma unroll
+            for (int i = 0; i < DT; ++i) mat_mul<T>(a.o[i], token_columns<T, across_pitch<T, KS>()>(vt, i, j, lane), w);
+        }
     }
 }
 __device__ __forceinline__ float attend_share(float l) { return l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l); }          // (no token: 0; NaN stays NaN)
@@ -296,8 +312,8 @@ inline size_t resident_bytes(int L, int row, int waves, int map) {
 }
 __device__ __forceinline__ char* resident_map(char* lds, int rows, int row, int wave, int map) { return lds + rows * row + (((rows / 32 + 2) * 4 + 15) & ~15) + wave * map; }
 
-template <typename T, int KS, int WAVES, bool RESIDENT>
-__global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_waves(sizeof(T) == 4, KS) : (sizeof(T) == 2 || KS <= 5 ? 2 : 1)) attend_kernel(const AttendParams p) {
+template <typename T, int KS, int WAVES, bool RESIDENT, bool BOTH = false>
+__global__ void __launch_bounds__(64 * WAVES, BOTH ? (KS <= 4 ? 3 : 2) : RESIDENT ? attend_waves(sizeof(T) == 4, KS) : (sizeof(T) == 2 || KS <= 5 ? 2 : 1)) attend_kernel(const AttendParams p) {
     using S = AttendShape<T, KS>;
     using Map = MapTile<T, KS>;
     constexpr int DT = (KS + 1) / 2;
@@ -350,7 +366,7 @@ __global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_waves(sizeof(T) 
             a.start();
             for (int i = 0; i < rows / 32; ++i) {
                 const uint32_t word = __builtin_amdgcn_readfirstlane(words[i]);
-                if (word) attend_tokens<T, KS>(lds + i * 32 * S::K_ROW, vt + i * 32 * S::V_ROW, word, q, a, c2, lane);
+                if (word) attend_tokens<T, KS, BOTH>(lds + i * 32 * S::K_ROW, vt + i * 32 * S::V_ROW, word, q, a, c2, lane);
             }
             finish(a, at, n, buf);
         }
@@ -377,7 +393,7 @@ __global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_waves(sizeof(T) 
 #pragma unroll
             for (int i = 0; i < S::TB / 32; ++i) {
                 const uint32_t word = (uint32_t)(in >> (32 * i));
-                if (word) attend_tokens<T, KS>(kt + 32 * i * S::K_ROW, vt + 32 * i * S::V_ROW, word, q, a, c2, lane);
+                if (word) attend_tokens<T, KS, BOTH>(kt + 32 * i * S::K_ROW, vt + 32 * i * S::V_ROW, word, q, a, c2, lane);
             }
         }
         finish(a, plane, n0, buf);
@@ -395,8 +411,8 @@ template <typename T, int KS> struct AttendFewShape {
     static constexpr int LDS = BUFFERS * STAGE > JOIN ? BUFFERS * STAGE : JOIN;
     static constexpr bool AHEAD = sizeof(T) == 2 || KS <= 4;         // (fp32: no registers for a stage on its way beside wide heads)
 };
-template <typename T, int KS>
-__global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS <= 5 : KS <= 4) ? 2 : 1) attend_few_kernel(const AttendParams p) {
+template <typename T, int KS, bool BOTH>
+__global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS <= 4 + !BOTH : KS <= 4) ? 2 : 1) attend_few_kernel(const AttendParams p) {
     using S = AttendFewShape<T, KS>;
     constexpr int TB = S::TB, DT = S::DT;
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -436,7 +452,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS <= 5 : KS <= 4) ? 2 
             if (S::AHEAD && st + 1 < last) next.fetch(p, b, head, (st + 1) * TB, tid);
             lds_barrier();
             const uint32_t word = (uint32_t)(in >> (wave & 1) * 32);
-            if (word) attend_tokens<T, KS>(kt + wave * 32 * S::K_ROW, vt + wave * 32 * S::V_ROW, word, q, a, c2, lane);
+            if (word) attend_tokens<T, KS, BOTH>(kt + wave * 32 * S::K_ROW, vt + wave * 32 * S::V_ROW, word, q, a, c2, lane);
         }
     }
     a.sum = other_half_sum(a.sum);
@@ -628,9 +644,14 @@ __global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_grad_waves(sizeo
             float x[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) { x[r] = e[8 * j + r] * (dp[8 * j + r] - delta); off += x[r]; }
-            const MatFrag<T> ds = mat_from_acc<T>(x);
+            MatFrag<T> ds, rest;
+            mat_split<T>(x, ds, rest);
 #pragma unroll
-            for (int i = 0; i < DT; ++i) mat_mul<T>(acc[i], token_columns<T, S::ROW>(kt, i, j, lane), ds);
+            for (int i = 0; i < DT; ++i) {
+                const MatFrag<T> k = token_columns<T, S::ROW>(kt, i, j, lane);
+                mat_mul<T>(acc[i], k, ds);
+                if constexpr (sizeof(T) == 2) mat_mul<T>(acc[i], k, rest);
+            }
         }
     };
     auto finish = [&](size_t at, int n, char* buf) {
@@ -745,8 +766,9 @@ template <typename T, int PX, int PITCH> __device__ __forceinline__ MatFrag<T> m
 }
 
 template <typename T, int KS, int WT>
-__global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS < 5 || (KS == 5 && WT > 1) : KS <= 3) ? 2 : 1) attend_grad_tokens_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS < 5 || (KS == 5 && WT == 4) : KS <= 3) ? 2 : 1) attend_grad_tokens_kernel(const AttendParams p) {
     using S = AttendTokenShape<T, KS, WT>;
+    constexpr bool SPLIT = sizeof(T) == 2 && WT < 4;                 // (fewer token waves: few tokens, and some other numbers of them)
     constexpr int DT = (KS + 1) / 2, PX = S::PX, PITCH = S::PITCH, E = 16 / (int)sizeof(T), PIECES = PX / E, ALL = KS * 16 * PIECES, COUNT = (ALL + 255) / 256;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -852,11 +874,20 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS < 5 || (KS == 5 && W
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const MatFrag<T> fe = mat_from_acc<T>(e + 8 * j), fd = mat_from_acc<T>(ds + 8 * j);
+                MatFrag<T> fe, fd, re, rd;
+                if constexpr (SPLIT) {
+                    mat_split<T>(e + 8 * j, fe, re);
+                    mat_split<T>(ds + 8 * j, fd, rd);
+                } else {
+                    fe = mat_from_acc<T>(e + 8 * j);
+                    fd = mat_from_acc<T>(ds + 8 * j);
+                }
 #pragma unroll
                 for (int i = 0; i < DT; ++i) {
-                    mat_mul<T>(av[i], map_rows<T, PX, PITCH>(tg, i, p0, j, lane), fe);
-                    mat_mul<T>(ak[i], map_rows<T, PX, PITCH>(tq, i, p0, j, lane), fd);
+                    const MatFrag<T> g = map_rows<T, PX, PITCH>(tg, i, p0, j, lane), x = map_rows<T, PX, PITCH>(tq, i, p0, j, lane);
+                    mat_mul<T>(av[i], g, fe);
+                    mat_mul<T>(ak[i], x, fd);
+                    if constexpr (SPLIT) { mat_mul<T>(av[i], g, re); mat_mul<T>(ak[i], x, rd); }
                 }
             }
         }
@@ -899,13 +930,18 @@ template <typename K> hipError_t attend_launch(K kernel, size_t items, int threa
 template <typename T, int KS> hipError_t launch_attend_many(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
     const size_t groups = (size_t)p.B * p.kv;
     if (plan.waves == 8) return attend_launch(attend_kernel<T, KS, 8, true>, groups * p.workers, 512, plan.lds, p, s);
+    if constexpr (sizeof(T) == 2) {
+        if (plan.resident && p.L <= SPLIT_MOST) return attend_launch(attend_kernel<T, KS, 4, true, true>, groups * p.workers, 256, plan.lds, p, s);
+    }
     if (plan.resident) return attend_launch(attend_kernel<T, KS, 4, true>, groups * p.workers, 256, plan.lds, p, s);
     return attend_launch(attend_kernel<T, KS, 4, false>, groups * p.workers, 256, AttendShape<T, KS>::LDS, p, s);
 }
 template <typename T, int KS> hipError_t launch_attend_head(const AttendParams& p, const AttendPlan& plan, hipStream_t s) {
     if (plan.few) {
         const size_t tiles = ((size_t)p.per * p.N + 31) / 32;
-        hipError_t e = attend_launch(attend_few_kernel<T, KS>, (size_t)p.B * p.kv * tiles * p.splits, 256, AttendFewShape<T, KS>::LDS, p, s);
+        auto kernel = attend_few_kernel<T, KS, false>;
+        if constexpr (sizeof(T) == 2) { if (p.L <= SPLIT_MOST) kernel = attend_few_kernel<T, KS, true>; }
+        hipError_t e = attend_launch(kernel, (size_t)p.B * p.kv * tiles * p.splits, 256, AttendFewShape<T, KS>::LDS, p, s);
         if (e != hipSuccess || p.splits == 1) return e;
         return attend_launch(attend_join_kernel<T>, (size_t)p.B * p.kv * tiles * ((p.D + 7) / 8), 256, (p.splits + 8) * 32 * 4, p, s);
     }

@@ -49,6 +49,17 @@ template <typename T> __device__ __forceinline__ MatFrag<T> mat_from_acc(const f
     return f;
 }
 
+// ... as two operands, the rounded values and what the rounding left (rounded in its turn): their products add up to that of some twice as many bits
+template <typename T> __device__ __forceinline__ void mat_split(const float* v, MatFrag<T>& hi, MatFrag<T>& lo) {
+    hi = mat_from_acc<T>(v);
+    if constexpr (sizeof(T) == 2) {
+        float rest[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rest[i] = v[i] - rg_elem<T>(hi.w, i);
+        lo = mat_from_acc<T>(rest);
+    }
+}
+
 typedef __attribute__((address_space(3))) char lds_char;
 // (an LDS pointer in its own address space, for the instructions that take no other)
 __device__ __forceinline__ lds_char* lds_ptr(const void* p) { return (lds_char*)(__attribute__((address_space(3))) void*)(void*)p; }
