@@ -30,14 +30,15 @@ void plan_positions(AttendPlan& a, const AttendParams& p, int row_bytes, int sim
 
 }  // namespace
 
-// Where the positions are less than three waves for every CU, the waves of a workgroup share 32 positions and take the tokens apart.  Few of those workgroups and
-// many tokens: stretches of the tokens, joined by a launch of their own.
+// Where the positions are less than three waves for every CU, the waves of a workgroup share 32 positions and take the tokens apart -- from more than 128 tokens
+// on, or on maps of less than a tile (6 heads of 64 channels, 14x14, 77 tokens: 7.1 us so, 5.5 a wave per tile; 20 positions of 12 fp32 heads,
+// 60 tokens: 7.6, 10.9).  Few of those workgroups and many tokens: stretches of the tokens, joined by a launch of their own.
 AttendPlan attend_plan(const AttendParams& p, int dtype) {
     AttendPlan a = {};
     const int ks = steps_of(p), es = dtype == 0 ? 4 : 2;
     const size_t groups = (size_t)p.B * p.kv, columns = (size_t)p.per * p.N;
     a.splits = 1;
-    if ((size_t)p.B * p.heads * ((p.N + 31) / 32) >= 768) {
+    if ((size_t)p.B * p.heads * ((p.N + 31) / 32) >= 768 || (p.L <= 128 && p.N >= 32)) {
         const int dt = (ks + 1) / 2, across = es == 4 ? dt * 128 + 32 : (dt % 2 ? dt * 64 : dt * 64 + 64);
         const bool both = es == 2 && p.L <= SPLIT_MOST;
         plan_positions(a, p, ks * 16 * es + 16 + across, both ? (ks <= 4 ? 3 : 2) : attend_waves(dtype == 0, ks), !both, dtype);

@@ -408,7 +408,11 @@ template <typename T, int KS> struct AttendFewShape {
     static constexpr int K_ROW = along_pitch<T, KS>(), V_ROW = across_pitch<T, KS>(), STAGE = TB * (K_ROW + V_ROW);
     static constexpr int BUFFERS = 2 * STAGE <= 160 * 1024 ? 2 : 1;
     static constexpr int JOIN = 4 * (DT * 32 + 2) * 32 * 4;
-    static constexpr int LDS = BUFFERS * STAGE > JOIN ? BUFFERS * STAGE : JOIN;
+    // (a stretch of one stage needs one buffer: more workgroups on a CU)
+    static int lds(int L, int splits) {
+        const int need = ((L + TB - 1) / TB <= splits ? 1 : BUFFERS) * STAGE;
+        return need > JOIN ? need : JOIN;
+    }
     static constexpr bool AHEAD = sizeof(T) == 2 || KS <= 4;         // (fp32: no registers for a stage on its way beside wide heads)
 };
 template <typename T, int KS, bool BOTH>
@@ -941,7 +945,7 @@ template <typename T, int KS> hipError_t launch_attend_head(const AttendParams& 
         const size_t tiles = ((size_t)p.per * p.N + 31) / 32;
         auto kernel = attend_few_kernel<T, KS, false>;
         if constexpr (sizeof(T) == 2) { if (p.L <= SPLIT_MOST) kernel = attend_few_kernel<T, KS, true>; }
-        hipError_t e = attend_launch(kernel, (size_t)p.B * p.kv * tiles * p.splits, 256, AttendFewShape<T, KS>::LDS, p, s);
+        hipError_t e = attend_launch(kernel, (size_t)p.B * p.kv * tiles * p.splits, 256, AttendFewShape<T, KS>::lds(p.L, p.splits), p, s);
         if (e != hipSuccess || p.splits == 1) return e;
         return attend_launch(attend_join_kernel<T>, (size_t)p.B * p.kv * tiles * ((p.D + 7) / 8), 256, (p.splits + 8) * 32 * 4, p, s);
     }

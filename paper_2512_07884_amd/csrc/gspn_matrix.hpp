@@ -83,13 +83,24 @@ __device__ __forceinline__ u32x2 lds_turned(const char* p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)lds_ptr(p)));
 }
 
+// a 16-byte piece moved down by s elements (0 .. all but one), zeros behind
+template <typename T> __device__ __forceinline__ u32x4 piece_down(u32x4 v, int s) {
+    uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+    const int bits = s * 8 * (int)sizeof(T);
+    if (bits >= 64) { lo = hi; hi = 0; }
+    const int b = bits & 63;
+    lo = lo >> b | (hi << 1) << (63 - b);
+    hi = hi >> b;
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
 // 16 bytes of a row from element `at` on, zeros from element `limit` on; every access lies within the row
 template <typename T> __device__ __forceinline__ u32x4 row_chunk(const T* row, int at, int limit) {
     constexpr int E = 16 / (int)sizeof(T);
     u32x4 v = {0, 0, 0, 0};
     if (at + E <= limit) v = rg_load(row + at);
     else if (at < limit) {
-        if (limit >= E) v = rg_realign<T>(rg_load(row + (limit - E)), at - (limit - E));
+        if (limit >= E) v = piece_down<T>(rg_load(row + (limit - E)), at - (limit - E));
         else {
             if constexpr (sizeof(T) == 4) {
                 if (at + 0 < limit) v[0] = ((const uint32_t*)row)[at + 0];
