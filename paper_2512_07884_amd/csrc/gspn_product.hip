@@ -26,8 +26,8 @@ bool huge_tiles(const ProductParams& p, int form, bool gated, int images, int dt
 // 64x64 63 55, 1152 x 1152 (not three quarters) 44 51; fp32 2048 x 256 on eight 32x32 87 77, 1152 x 144 on two 64x64 68 44.
 bool medium_gradient(const ProductParams& p) {
     const size_t tiles = tiles_of(p, false, 64, 64, 1);
-    // (its stages are 128 pixels of an image, the larger tile's 32: 768 x 768 on 64 maps of 7x7 156 us and 50)
-    if ((p.K + 127) / 128 * 4 * 2 > (p.K + 31) / 32 * 3) return false;
+    // (its stages are 64 pixels of an image, the larger tile's 32)
+    if ((p.K + 63) / 64 * 2 * 2 > (p.K + 31) / 32 * 3) return false;
     return p.M <= 64 || p.N <= 64 || (tiles <= 512 && 512 / tiles * tiles >= 384);
 }
 // Large tiles where there are two for every CU; flat ones where there are nearly as many of those; smaller ones, with several waves over the contracted axis,

@@ -537,10 +537,10 @@ template <typename T, int FORM, int OUTC> hipError_t launch_product_as(const Pro
             if constexpr (sizeof(T) == 2)
                 return launch_product_tile<T, FORM, OUTC, 2, 2, 4, 4, 1, 128, 2, true>(p, s);
         case TILE_LARGE: return launch_product_tile<T, FORM, OUTC, 2, 2, 2, 2, 1, 64, 2>(p, s);
-        case TILE_MEDIUM: return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 2, 2>(p, s);
-        case TILE_SMALL: return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 1, 4>(p, s);
+        case TILE_MEDIUM: return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 2, 2, 64, 2>(p, s);
+        case TILE_SMALL: return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 1, 4, 64, 2>(p, s);
         default:
-            if constexpr (OUTC == OUT_GATED || OUTC == OUT_GATED_GRAD) return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 4, 1>(p, s);
+            if constexpr (OUTC == OUT_GATED || OUTC == OUT_GATED_GRAD) return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 4, 1, 64, 2>(p, s);
             else return launch_product_tile<T, FORM, OUTC, 1, 1, 1, 4, 1>(p, s);
     }
 }
