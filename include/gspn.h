@@ -254,7 +254,8 @@ enum { GSPN_ACT_NONE = 0, GSPN_ACT_SILU = 1, GSPN_ACT_GELU = 2, GSPN_ACT_SIGMOID
  * with a bias; the way back up with the block's residual):
  *     out[b][m][n] = act(sum_k P[m][k] in[b][k][n] + bias[m]) + residual[b][m][n]          n = pixel
  *   in [B,K,H,W]; P [M,K]; bias [M] or NULL; residual [B,M,H,W] or NULL; out [B,M,H,W]
- * A matrix of 2^31 or more values, and maps whose tiles no launch counts, are GSPN_ERR_UNSUPPORTED. */
+ * A matrix of 2^31 or more values is GSPN_ERR_UNSUPPORTED, and so are maps of which a launch cannot count the tiles: 2^24 or more of 32 rows of P (in the
+ * backward call: of P or of in) by 128 pixels (32, in maps of fewer than 128). */
 int gspn_proxy_project_fused(const void* in, const void* P, const void* bias, const void* residual, void* out,
                              int B, int K, int M, int H, int W, int act, int dtype, void* stream);
 /* Its gradients, given gout = dL/dout.  Nothing is kept from the forward call: with an activation the product is computed again.
@@ -288,8 +289,9 @@ unsigned long long gspn_gated_project_bwd_bytes(int B, int K, int F, int H, int 
  *   mask   [B,L] bytes, 0: the token takes no part (whatever k and v hold for it is never used); NULL: all take part
  *   lse    [B,heads,H,W] fp32, log of the sum of exp(s), for the backward call; or NULL
  * A position whose image has no token that takes part gets out = 0 and lse = -inf.  heads must be a multiple of kv_heads, scale positive and finite (else
- * GSPN_ERR_SHAPE); D a multiple of 8 and at most GSPN_MAX_HEAD, L at most GSPN_MAX_TOKENS (else GSPN_ERR_UNSUPPORTED).  The weights p are
- * rounded to the storage type for the product with v; the sums of both are fp32.
+ * GSPN_ERR_SHAPE); D a multiple of 8 and at most GSPN_MAX_HEAD, L at most GSPN_MAX_TOKENS (else GSPN_ERR_UNSUPPORTED).  So are maps of 2^26 or
+ * more positions, and B*heads*H*W or B*kv_heads*L too large for the workgroups of a launch (2^27, 2^29).  The weights p are rounded to the storage type for
+ * the product with v (of up to 64 tokens it takes what that rounding left as well); the sums of both are fp32.
  *   workspace: calls of few positions and many tokens cut the tokens into stretches, given gspn_cross_attention_bytes bytes (0: no use for any) of device
  *   memory under the terms above; NULL: the same result up to rounding, without the stretches. */
 enum { GSPN_MAX_HEAD = 128, GSPN_MAX_TOKENS = 1 << 24 };
@@ -301,7 +303,8 @@ unsigned long long gspn_cross_attention_bytes(int B, int heads, int kv_heads, in
  *     ds = p * (sum_d v gout - sum_d gout out);  gq = scale sum_t ds k;  gk = scale sum ds q;  gv = sum p gout   (gk, gv over the positions of all heads
  *     that share the token's head; 0 for tokens that take no part)
  *   gq [B,heads*D,H,W], gk, gv [B,L,kv_heads*D]: out, or NULL (not computed; one of them at least); workspace (required) of
- *   gspn_cross_attention_bwd_bytes bytes under the terms above.  p and ds are rounded to the storage type for the products.  No atomics. */
+ *   gspn_cross_attention_bwd_bytes bytes under the terms above.  p and ds are rounded to the storage type for the products (gq takes what the
+ *     rounding of ds left as well).  No atomics: the result is bitwise repeatable. */
 int gspn_cross_attention_bwd(const void* gout, const void* q, const void* k, const void* v, const unsigned char* mask, const void* out, const float* lse,
                              void* gq, void* gk, void* gv, void* workspace, unsigned long long workspace_bytes,
                              int B, int heads, int kv_heads, int D, int H, int W, int L, float scale, int dtype, void* stream);

@@ -13,6 +13,12 @@ size_t storage(int dtype) { return dtype == GSPN_F32 ? 4 : 2; }
 size_t rounded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 constexpr long long TOP = 1ll << 31;
 
+// A launch counts the workgroups of a result of `rows` rows and N pixels: 32 pixels of short rows each at least, 128 of others (narrower ones are taken where they are few)
+bool counted(long long B, long long rows, long long N) {
+    const long long columns = N < 128 ? N / 32 + 1 : N / 128 + 1;
+    return columns * B < TOP / 128 && columns * B * (rows / 32 + 1) < TOP / 128;
+}
+
 // rows: rows of P (M, or 2 F of the gated pair)
 int check_product(int B, int K, int M, int rows_per, int H, int W, int act, int dtype) {
     if (B < 1 || K < 1 || M < 1 || H < 1 || W < 1) return GSPN_ERR_SHAPE;
@@ -20,10 +26,8 @@ int check_product(int B, int K, int M, int rows_per, int H, int W, int act, int 
     if (!known_act(act)) return GSPN_ERR_UNSUPPORTED;
     if (H > GSPN_MAX_LINE || W > GSPN_MAX_LINE) return GSPN_ERR_UNSUPPORTED;
     const long long rows = (long long)M * rows_per, N = (long long)H * W;
-    // sizes that a launch counts its workgroups and a kernel its rows with: maps and matrices of less than 2^31 values a side, an image's
-    // tiles and the batch's as well
-    if (rows >= TOP || N >= TOP || rows * K >= TOP || (N / 128 + 1) * B >= TOP / 128 || (N / 128 + 1) * B * (rows / 32 + 1) >= TOP / 128)
-        return GSPN_ERR_UNSUPPORTED;
+    // maps and matrices of less than 2^31 values a side
+    if (rows >= TOP || N >= TOP || rows * K >= TOP || !counted(B, rows, N)) return GSPN_ERR_UNSUPPORTED;
     return GSPN_OK;
 }
 
@@ -43,6 +47,14 @@ ProductParams matrix_params(int B, int K, int rows, int N) {
     p.M = rows; p.N = K; p.K = N; p.images = B; p.splits = 1;
     return p;
 }
+// What the backward call launches besides: results of K rows, of rows x K, and the sums over rows
+int check_product_back(int B, int K, int M, int rows_per, int H, int W, int act, int dtype) {
+    const int st = check_product(B, K, M, rows_per, H, W, act, dtype);
+    if (st != GSPN_OK) return st;
+    const long long rows = (long long)M * rows_per, N = (long long)H * W;
+    if (!counted(B, K, N) || (rows / 64 + 1) * (K / 64 + 1) >= TOP / 512 || (N / 4096 + 1) * B * M >= TOP / 32) return GSPN_ERR_UNSUPPORTED;
+    return GSPN_OK;
+}
 ProductBack back_layout(int B, int K, int M, bool gated, int N, int act, int dtype) {
     ProductBack w = {};
     const int rows = gated ? 2 * M : M;
@@ -59,7 +71,7 @@ ProductBack back_layout(int B, int K, int M, bool gated, int N, int act, int dty
 int product_backward(const void* gout, const void* in, const void* P, const void* bias, void* gin, void* gP, void* gbias, void* workspace,
                      unsigned long long workspace_bytes, int B, int K, int M, bool gated, int H, int W, int act, int dtype, void* stream) {
     if (!gout || !in || !P || (!gin && !gP && !gbias) || !workspace) return GSPN_ERR_NULL;
-    const int st = check_product(B, K, M, gated ? 2 : 1, H, W, act, dtype);
+    const int st = check_product_back(B, K, M, gated ? 2 : 1, H, W, act, dtype);
     if (st != GSPN_OK) return st;
     if (off16(gout) || off16(in) || off16(P) || off16(bias) || off16(gin) || off16(gP) || off16(gbias) || off16(workspace)) return GSPN_ERR_ALIGN;
     const int N = H * W, rows = gated ? 2 * M : M;
@@ -100,7 +112,8 @@ int check_attend(int B, int heads, int kv_heads, int D, int H, int W, int L, flo
     if (H > GSPN_MAX_LINE || W > GSPN_MAX_LINE || D % 8 != 0 || D > GSPN_MAX_HEAD || L > GSPN_MAX_TOKENS) return GSPN_ERR_UNSUPPORTED;
     // workgroups of a launch: 32 positions each at least
     const long long N = (long long)H * W, per = heads / kv_heads;
-    if (N >= TOP / 32 || per * N >= TOP / 4 || (long long)B * kv_heads >= TOP / 1024 || (long long)B * kv_heads * (per * N / 32 + 1) >= TOP / 128 || (long long)B * heads * N >= TOP / 16)
+    if (N >= TOP / 32 || per * N >= TOP / 4 || (long long)B * kv_heads >= TOP / 1024 || (long long)B * kv_heads * (per * N / 32 + 1) >= TOP / 128 || (long long)B * heads * N >= TOP / 16 ||
+        (long long)B * kv_heads * (L / 32 + 1) >= TOP / 128)
         return GSPN_ERR_UNSUPPORTED;
     return GSPN_OK;
 }
@@ -184,12 +197,12 @@ int gspn_gated_project(const void* in, const void* P, const void* bias, void* ou
 }
 
 unsigned long long gspn_proxy_project_fused_bwd_bytes(int B, int K, int M, int H, int W, int act, int dtype) {
-    if (check_product(B, K, M, 1, H, W, act, dtype) != GSPN_OK) return 0;
+    if (check_product_back(B, K, M, 1, H, W, act, dtype) != GSPN_OK) return 0;
     return back_layout(B, K, M, false, H * W, act, dtype).bytes;
 }
 
 unsigned long long gspn_gated_project_bwd_bytes(int B, int K, int F, int H, int W, int act, int dtype) {
-    if (check_product(B, K, F, 2, H, W, act, dtype) != GSPN_OK) return 0;
+    if (check_product_back(B, K, F, 2, H, W, act, dtype) != GSPN_OK) return 0;
     return back_layout(B, K, F, true, H * W, act, dtype).bytes;
 }
 

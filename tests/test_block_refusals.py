@@ -53,6 +53,20 @@ def test_products_refuse_on_the_host(lib):
     assert lib.gspn_proxy_project_fused(p, p, p, odd, p, *dims, 1, 1, None) == ALIGN           # the residual
 
 
+def test_sizes_that_no_launch_counts(lib):
+    """Refused before anything is launched, the backward call's other launches included; what is just below has a workspace's size."""
+    def back(*d, act=1):
+        return lib.gspn_proxy_project_fused_bwd(p, p, p, p, p, p, p, p, 1 << 62, *d, act, 1, None)
+    for act, sizes in ((1, [(1 << 24, 8, 8, 5, 8), (1 << 20, 1024, 8, 1, 1), (1, 1 << 30, 1, 1, 1)]), (0, [(1 << 22, 8, 32, 1, 1)])):
+        for d in sizes:
+            assert back(*d, act=act) == UNSUPPORTED and lib.gspn_proxy_project_fused_bwd_bytes(*d, act, 1) == 0, d
+    assert lib.gspn_proxy_project_fused_bwd_bytes(1 << 18, 1024, 8, 1, 1, 1, 1) > 0
+    assert lib.gspn_proxy_project_fused_bwd_bytes(1 << 22, 8, 8, 5, 8, 1, 1) > 0
+    assert lib.gspn_proxy_project_fused(p, p, p, p, p, 1 << 24, 8, 8, 5, 8, 1, 1, None) == UNSUPPORTED
+    tokens = (64, 64, 64, 8, 1, 1, 1 << 24)
+    assert lib.gspn_cross_attention(p, p, p, p, p, p, p, 1 << 62, *tokens, 0.3, 1, None) == UNSUPPORTED
+
+
 def test_attention_refuses_on_the_host(lib):
     dims = (2, 4, 2, 16, 5, 7, 33)
     big = 1 << 40
