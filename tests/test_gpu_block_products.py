@@ -70,6 +70,24 @@ def test_tiles_of_many(shape, dtype):
         _case(*shape, dtype, "gelu", True, False, True, 61)
 
 
+# every tile with several stages, in 16-byte requests straight to LDS and (odd rows) through registers; 256x256 for the result, the map's gradient and the
+# matrix's; 128x128, 64x64 and 64x32; stretches of the pixels over several images
+TILES = [(3, 1024, 1024, 64, 64), (1, 3584, 3584, 16, 16), (4, 1152, 1152, 28, 28), (8, 512, 1024, 31, 33), (8, 512, 1024, 32, 32), (20, 96, 96, 56, 56), (20, 96, 96, 55, 57),
+         (8, 384, 384, 14, 14), (8, 384, 384, 13, 15), (64, 200, 136, 7, 7), (2, 300, 200, 7, 9)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("shape", TILES, ids=lambda s: "x".join(map(str, s)))
+def test_every_tile(shape, dtype):
+    _case(*shape, dtype, "silu", True, True, False, 70)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(3, 512, 512, 64, 64), (8, 512, 512, 31, 33), (20, 96, 48, 56, 56), (8, 384, 192, 13, 15), (32, 200, 100, 7, 7)], ids=lambda s: "x".join(map(str, s)))
+def test_every_tile_of_the_gated_pair(shape, dtype):
+    _case(*shape, dtype, "gelu", True, False, True, 71)
+
+
 def test_large_values_of_the_activations():
     """Far from zero the activations are 0, z or 1, without infinities or NaN."""
     import paper_2512_07884_amd as G

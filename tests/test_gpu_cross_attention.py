@@ -92,6 +92,15 @@ def test_forms(shape, D, dtype):
     _case(B, heads, kv, D, H, W, L, dtype, "padded", D, step=D in (16, 64) or H < 40)
 
 
+# many positions: a head's tokens in LDS for four and eight waves with several turns, and more tokens than LDS holds (16 bits: D 128, 300 of them), in both calls;
+# odd positions, positions short of a wave's 32
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("shape", [(2, 16, 16, 128, 32, 32, 300), (2, 16, 4, 128, 31, 33, 301), (2, 16, 8, 64, 47, 47, 200), (1, 32, 32, 104, 27, 31, 700),
+                                   (4, 16, 16, 32, 31, 31, 90), (1, 8, 4, 104, 3, 5, 700)], ids=str)
+def test_tokens_in_lds_and_streamed(shape, dtype):
+    _case(*shape, dtype, "padded", shape[6], step=True)
+
+
 @pytest.mark.parametrize("per", [1, 2, 4, 7])
 @pytest.mark.parametrize("positions", [1, 5, 33])
 def test_few_positions_over_many_tokens(per, positions):
