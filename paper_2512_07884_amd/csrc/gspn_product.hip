@@ -22,19 +22,19 @@ bool huge_tiles(const ProductParams& p, int form, bool gated, int images, int dt
     return used >= 0.75 || (used >= 0.6 && p.K >= 2048);
 }
 // The gradient of the matrix: 64 x 64 where those, with the pixels cut into as many stretches as make two workgroups for every CU, use three quarters of them.
-// 128 x 128 and 64 x 64, each at its best number of stretches (us): bf16 512 x 512 on two 64x64 maps 27 18, 1536 x 384 on four 32x32 26 20, 2048 x 1024 on two
-// 64x64 63 55, 1152 x 1152 (not three quarters) 44 51; fp32 2048 x 256 on eight 32x32 87 77, 1152 x 144 on two 64x64 68 44.
+// 128 x 128 at its best number of stretches and 64 x 64 as chosen (us): bf16 512 x 512 on two 64x64 maps 27 18, 1536 x 384 on four 32x32 26 17, 2048 x 1024 on two
+// 64x64 62 52, 1152 x 1152 (not three quarters) 44 51; fp32 2048 x 256 on eight 32x32 87 71, 1152 x 144 on two 64x64 68 38.
 bool medium_gradient(const ProductParams& p) {
     const size_t tiles = tiles_of(p, false, 64, 64, 1);
-    // (its stages are 64 pixels of an image, the larger tile's 32)
-    if ((p.K + 63) / 64 * 2 * 2 > (p.K + 31) / 32 * 3) return false;
+    // (its stages are 128 pixels of an image, the larger tile's 32: of small images most of them would be empty)
+    if ((p.K + 127) / 128 * 4 * 2 > (p.K + 31) / 32 * 3) return false;
     return p.M <= 64 || p.N <= 64 || (tiles <= 512 && 512 / tiles * tiles >= 384);
 }
 // Large tiles where there are two for every CU; flat ones where there are nearly as many of those; smaller ones, with several waves over the contracted axis,
 // where there are not.  Rows of fewer pixels than a tile has columns are requested piece by piece, so a narrower tile comes first.
-// Times (us) on 128 x 128, 32 x 128, 64 x 64, 64 x 32 tiles: bf16 1152 x 144 on two 64x64 maps 13 14 20 58, 384 x 384 on eight 28x28 13 9 11 21, 144 x 1152 on two
-// 64x64 22 12 10 20, 512 x 512 on one 33x33 15 9 8 11, 768 x 768 on 64 of 7x7 56 92 54 34; fp32 1024 x 1024 on two 64x64 135 - - -, 96 x 96 on 64 of
-// 56x56 71 51 93 196, 384 x 384 on eight 28x28 32 24 27 33, 96 x 384 on one 14x14 31 11 11 8.
+// Times (us) on 128 x 128, 32 x 128, 64 x 64, 64 x 32 tiles: bf16 1152 x 144 on two 64x64 maps 13 14 14 25, 384 x 384 on eight 28x28 13 9 9 12, 144 x 1152 on two
+// 64x64 23 12 12 13, 512 x 512 on one 33x33 15 9 8 8, 768 x 768 on 64 of 7x7 38 57 22 20, 1024 x 1024 on two 64x64 26 34 32 52; fp32 1024 x 1024 on two
+// 64x64 135 136 142 149, 96 x 96 on 64 of 56x56 72 52 65 111, 384 x 384 on eight 28x28 32 25 24 24, 96 x 384 on one 14x14 30 10 11 8.
 int product_tile(const ProductParams& p, int form, int outcome, int dtype) {
     const bool gated = outcome == OUT_GATED || outcome == OUT_GATED_GRAD;
     if (form == PRODUCT_GRAD_MATRIX) return medium_gradient(p) ? TILE_MEDIUM : (huge_tiles(p, form, false, 1, dtype) ? TILE_HUGE : TILE_LARGE);

@@ -3,9 +3,10 @@
 //
 //     R[m][n] = sum_k A[m][k] B[k][n]
 //
-// A workgroup owns a tile of BM x BN results and walks the contracted axis in stages of WK times 128 bytes.  Both operands of a stage
-// go through LDS: requests of 16 bytes that run along the rows as they are stored, two stages of LDS, the stage after them on its way in
-// registers while the waves multiply.  An operand whose contracted axis is contiguous is read from LDS 16 bytes per lane; one whose rows run
+// A workgroup owns a tile of BM x BN results and walks the contracted axis in stages of WK times 64 or 128 bytes.  Both operands of a stage
+// go through LDS in requests of 16 bytes that run along the rows as they are stored, into NBUF stages of LDS: straight from memory where the rows are whole
+// 16-byte pieces and at least a tile long, else through registers, the next stage on its way while the waves multiply (1024 x 1024 channels on 64x64 maps and on
+// 63x65 ones, bf16: 26.3 and 30.6 us).  An operand whose contracted axis is contiguous is read from LDS 16 bytes per lane; one whose rows run
 // across it (the pixels of the maps) is turned on the way out of LDS (ds_read_b64_tr_b16; fp32: single words).  Both are stored with the
 // 16-byte pieces of a row exchanged by the row's number, so that neither the rows nor the columns that a request touches share banks.
 // The waves stand WM x WN over the tile and WK over the stage (small results, where tiles are few: the sums of the WK waves meet in LDS).
@@ -531,17 +532,21 @@ hipError_t launch_product_tile(const ProductParams& p, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Bytes of a row in a stage: 64, which leaves room for more workgroups on a CU, but 128 for flat tiles of one row block (fewer turns; 64 is less than a request per
+// thread) and 256 x 256, and for the 64 x 64 tiles of the matrix's gradient, which read both operands along their rows (512 x 512 on two 64x64 maps in
+// bf16, at the best number of stretches: 18 us, with 64 bytes 21).
 template <typename T, int FORM, int OUTC> hipError_t launch_product_as(const ProductParams& p, int tile, hipStream_t s) {
-    switch (tile) {
-        case TILE_HUGE:
-            if constexpr (sizeof(T) == 2)
-                return launch_product_tile<T, FORM, OUTC, 2, 2, 4, 4, 1, 128, 2, true>(p, s);
-        case TILE_LARGE: return launch_product_tile<T, FORM, OUTC, 2, 2, 2, 2, 1, 64, 2>(p, s);
-        case TILE_MEDIUM: return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 2, 2, 64, 2>(p, s);
-        case TILE_SMALL: return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 1, 4, 64, 2>(p, s);
-        default:
-            if constexpr (OUTC == OUT_GATED || OUTC == OUT_GATED_GRAD) return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 4, 1, 64, 2>(p, s);
-            else return launch_product_tile<T, FORM, OUTC, 1, 1, 1, 4, 1>(p, s);
+    if (tile == TILE_HUGE) {
+        if constexpr (sizeof(T) == 2) return launch_product_tile<T, FORM, OUTC, 2, 2, 4, 4, 1, 128, 2, true>(p, s);
+        else return hipErrorInvalidValue;               // (product_tile does not choose it)
+    }
+    if (tile == TILE_LARGE) return launch_product_tile<T, FORM, OUTC, 2, 2, 2, 2, 1, 64, 2>(p, s);
+    if constexpr (FORM == PRODUCT_GRAD_MATRIX) return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 2, 2>(p, s);
+    else {
+        if (tile == TILE_MEDIUM) return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 2, 2, 64, 2>(p, s);
+        if (tile == TILE_SMALL) return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 1, 4, 64, 2>(p, s);
+        if constexpr (OUTC == OUT_GATED || OUTC == OUT_GATED_GRAD) return launch_product_tile<T, FORM, OUTC, 2, 1, 1, 4, 1, 64, 2>(p, s);
+        else return launch_product_tile<T, FORM, OUTC, 1, 1, 1, 4, 1>(p, s);
     }
 }
 template <typename T> hipError_t launch_product_type(const ProductParams& p, int form, int outcome, int tile, hipStream_t s) {
