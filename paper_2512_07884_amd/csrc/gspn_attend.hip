@@ -67,10 +67,21 @@ AttendBackPlan attend_back_plan(const AttendParams& p, int dtype) {
     }
     const int px = a.token_waves == 1 ? 128 : 64;
     const size_t items = (size_t)p.B * p.kv * ((p.L + 32 * a.token_waves - 1) / (32 * a.token_waves));
-    const size_t stages = (size_t)((p.N + px - 1) / px) * p.per;
-    size_t n = (512 + items - 1) / items;
-    if (n > stages / 2) n = stages / 2;
-    a.splits = n < 1 ? 1 : (int)n;
+    const size_t stages = (size_t)((p.N + px - 1) / px) * p.per, room = 256 * (size_t)attend_token_groups(dtype == 0, ks, a.token_waves);
+    // Stretches of the positions: the chip's rounds of workgroups times the stages of one and two more for its start and end, at the least.  Stretches of fewer than
+    // four stages only while there are CUs without a workgroup (the sums of their results cost more than they gain).  The backward call with 512 workgroups
+    // or a few more, and by this rule: 16 heads of 72, two 64x64 maps, 300 tokens, f16 128 and 111 us, fp32 653 and 572; 8 heads of 128, 450 tokens, f16
+    // 145 and 134, fp32 703 and 671; 8 heads of 40, eight 32x32, 77 tokens, f16 29 and 26; 16 heads of 64, 77 tokens, f16 49 and 50, fp32 162 and 151.
+    const size_t idle = 256 / items < stages / 2 ? 256 / items : stages / 2;
+    size_t fewest = ~(size_t)0;
+    for (size_t rounds = 1; rounds <= 4; ++rounds) {
+        size_t n = rounds * room / items;
+        if (n > stages / 4) n = stages / 4;
+        if (n < idle) n = idle;
+        if (n < 1) n = 1;
+        const size_t cost = (items * n + room - 1) / room * ((stages + n - 1) / n + 2);
+        if (cost < fewest) { fewest = cost; a.splits = (int)n; }
+    }
     a.parts = a.splits * (4 / a.token_waves);
     a.delta_bytes = rounded((size_t)p.B * p.heads * p.N * sizeof(float));
     a.bytes = a.delta_bytes + (a.parts > 1 ? rounded(2 * (size_t)a.parts * p.B * p.L * p.kv * p.D * sizeof(float)) : 0);

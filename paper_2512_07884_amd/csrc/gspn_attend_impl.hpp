@@ -302,6 +302,8 @@ constexpr int RESIDENT_MOST = 160 * 1024;
 // of one file, none in the accumulation file that takes a move per value read.)
 constexpr int attend_waves(bool f32, int ks) { return f32 ? (ks <= 2 ? 4 : ks <= 3 ? 3 : 2) : (ks <= 4 ? 4 : ks <= 6 ? 3 : 2); }
 constexpr int attend_grad_waves(bool f32, int ks) { return f32 ? (ks <= 2 ? 3 : ks <= 5 ? 2 : 1) : (ks <= 2 ? 4 : 2); }
+// ... and workgroups of the kernel over the tokens on a CU (wt: waves along the tokens)
+constexpr int attend_token_groups(bool f32, int ks, int wt) { return (f32 ? ks <= 3 : ks < 5 || (ks == 5 && wt == 4)) ? 2 : 1; }
 // ... with the next tile of the maps in registers beside them; wide heads bring a tile when it is wanted, one map after the other
 constexpr bool attend_ahead(bool f32, int ks) { return !f32 || ks <= 6; }
 constexpr bool attend_grad_ahead(bool f32, int ks) { return f32 ? ks <= 3 : ks <= 6; }
@@ -770,7 +772,7 @@ template <typename T, int PX, int PITCH> __device__ __forceinline__ MatFrag<T> m
 }
 
 template <typename T, int KS, int WT>
-__global__ void __launch_bounds__(256, (sizeof(T) == 2 ? KS < 5 || (KS == 5 && WT == 4) : KS <= 3) ? 2 : 1) attend_grad_tokens_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(256, attend_token_groups(sizeof(T) == 4, KS, WT)) attend_grad_tokens_kernel(const AttendParams p) {
     using S = AttendTokenShape<T, KS, WT>;
     constexpr bool SPLIT = sizeof(T) == 2 && WT < 4;                 // (fewer token waves: few tokens, and some other numbers of them)
     constexpr int DT = (KS + 1) / 2, PX = S::PX, PITCH = S::PITCH, E = 16 / (int)sizeof(T), PIECES = PX / E, ALL = KS * 16 * PIECES, COUNT = (ALL + 255) / 256;
