@@ -254,7 +254,7 @@ enum { GSPN_ACT_NONE = 0, GSPN_ACT_SILU = 1, GSPN_ACT_GELU = 2, GSPN_ACT_SIGMOID
  * with a bias; the way back up with the block's residual):
  *     out[b][m][n] = act(sum_k P[m][k] in[b][k][n] + bias[m]) + residual[b][m][n]          n = pixel
  *   in [B,K,H,W]; P [M,K]; bias [M] or NULL; residual [B,M,H,W] or NULL; out [B,M,H,W]
- * A matrix of 2^31 or more values is GSPN_ERR_UNSUPPORTED, and so are maps of which a launch cannot count the tiles: 2^24 or more of 32 rows of P (in the
+ * A matrix of 2^31 or more values, or 2^30 or more channels, are GSPN_ERR_UNSUPPORTED, and so are maps of which a launch cannot count the tiles: 2^24 or more of 32 rows of P (in the
  * backward call: of P or of in) by 128 pixels (32, in maps of fewer than 128). */
 int gspn_proxy_project_fused(const void* in, const void* P, const void* bias, const void* residual, void* out,
                              int B, int K, int M, int H, int W, int act, int dtype, void* stream);

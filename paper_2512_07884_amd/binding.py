@@ -509,7 +509,7 @@ def _need(x, nbytes, workspace, stream, name):
             raise ValueError("workspace: must be a contiguous tensor on the device of the call's tensors")
         return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
     keep = _workspace(x, nbytes, stream) if nbytes else None
-    if keep is None and name is not None:
+    if keep is None and name is not None and nbytes:                  # (0: arguments that the call refuses)
         raise RuntimeError(f"{name}: no memory of torch's allocator for a workspace of {nbytes} bytes on this stream: pass one")
     return (None, 0, None) if keep is None else (keep.data_ptr(), nbytes, keep)
 
@@ -603,7 +603,7 @@ def _attend_args(q, k, v, mask, heads, kv_heads, scale):
 def _lse_ptr(lse, q, heads):
     B, _, H, W = q.shape
     torch = (_TORCH or _torch())[0]
-    if not lse.is_cuda or lse.device != q.device or lse.dtype != torch.float32 or tuple(lse.shape) != (B, heads, H, W) or not lse.is_contiguous():
+    if lse is None or not lse.is_cuda or lse.device != q.device or lse.dtype != torch.float32 or tuple(lse.shape) != (B, heads, H, W) or not lse.is_contiguous():
         raise ValueError(f"lse: must be a contiguous float32 device tensor of shape {(B, heads, H, W)}")
     return lse.data_ptr()
 

@@ -293,16 +293,16 @@ const char* gspn_status_string(int status) {
     switch (status) {
         case GSPN_OK: return "ok";
         case GSPN_ERR_NULL: return "a required pointer is NULL";
-        case GSPN_ERR_SHAPE: return "bad shape: dimensions and kchunk must be >= 1, C divisible by G, dir_mask in 1..15";
+        case GSPN_ERR_SHAPE: return "bad shape: dimensions and kchunk must be >= 1, C divisible by G, heads by kv_heads, dir_mask in 1..15, scale > 0, the workspace as large as asked for";
         case GSPN_ERR_DTYPE: return "dtype must be GSPN_F32, GSPN_BF16 or GSPN_F16";
         case GSPN_ERR_ALIGN: return "pointers must be 16-byte aligned";
-        case GSPN_ERR_UNSUPPORTED: return "unsupported: line longer than GSPN_MAX_LINE (GSPN_MAX_LINE_LOGITS with logits), unknown flag, or B*M*K beyond the static workspace";
+        case GSPN_ERR_UNSUPPORTED: return "unsupported: line longer than GSPN_MAX_LINE (GSPN_MAX_LINE_LOGITS with logits), unknown flag or activation, heads of other than 8, 16, .. GSPN_MAX_HEAD channels, sizes beyond a launch, or B*M*K beyond the static workspace";
         case GSPN_ERR_HIP: return "HIP launch failed";
         default: return "unknown status";
     }
 }
 
-int gspn_version(void) { return 300; }   // 0.3.0: testing aids read once (gspn_reload_env)
+int gspn_version(void) { return 400; }   // 0.4.0: the operators around the scan
 
 void gspn_reload_env(void) { reload_env_knobs(); }
 

@@ -27,7 +27,7 @@ int check_product(int B, int K, int M, int rows_per, int H, int W, int act, int 
     if (H > GSPN_MAX_LINE || W > GSPN_MAX_LINE) return GSPN_ERR_UNSUPPORTED;
     const long long rows = (long long)M * rows_per, N = (long long)H * W;
     // maps and matrices of less than 2^31 values a side
-    if (rows >= TOP || N >= TOP || rows * K >= TOP || !counted(B, rows, N)) return GSPN_ERR_UNSUPPORTED;
+    if (rows >= TOP || N >= TOP || K >= TOP / 2 || rows * K >= TOP || !counted(B, rows, N)) return GSPN_ERR_UNSUPPORTED;
     return GSPN_OK;
 }
 
@@ -70,9 +70,10 @@ ProductBack back_layout(int B, int K, int M, bool gated, int N, int act, int dty
 
 int product_backward(const void* gout, const void* in, const void* P, const void* bias, void* gin, void* gP, void* gbias, void* workspace,
                      unsigned long long workspace_bytes, int B, int K, int M, bool gated, int H, int W, int act, int dtype, void* stream) {
-    if (!gout || !in || !P || (!gin && !gP && !gbias) || !workspace) return GSPN_ERR_NULL;
+    if (!gout || !in || !P || (!gin && !gP && !gbias)) return GSPN_ERR_NULL;
     const int st = check_product_back(B, K, M, gated ? 2 : 1, H, W, act, dtype);
     if (st != GSPN_OK) return st;
+    if (!workspace) return GSPN_ERR_NULL;
     if (off16(gout) || off16(in) || off16(P) || off16(bias) || off16(gin) || off16(gP) || off16(gbias) || off16(workspace)) return GSPN_ERR_ALIGN;
     const int N = H * W, rows = gated ? 2 * M : M;
     const ProductBack w = back_layout(B, K, M, gated, N, act, dtype);
@@ -158,9 +159,10 @@ int gspn_cross_attention(const void* q, const void* k, const void* v, const unsi
 int gspn_cross_attention_bwd(const void* gout, const void* q, const void* k, const void* v, const unsigned char* mask, const void* out, const float* lse,
                              void* gq, void* gk, void* gv, void* workspace, unsigned long long workspace_bytes,
                              int B, int heads, int kv_heads, int D, int H, int W, int L, float scale, int dtype, void* stream) {
-    if (!gout || !q || !k || !v || !out || !lse || (!gq && !gk && !gv) || !workspace) return GSPN_ERR_NULL;
+    if (!gout || !q || !k || !v || !out || !lse || (!gq && !gk && !gv)) return GSPN_ERR_NULL;
     const int st = check_attend(B, heads, kv_heads, D, H, W, L, scale, dtype);
     if (st != GSPN_OK) return st;
+    if (!workspace) return GSPN_ERR_NULL;
     if (off16(gout) || off16(q) || off16(k) || off16(v) || off16(out) || off16(lse) || off16(gq) || off16(gk) || off16(gv) || off16(workspace))
         return GSPN_ERR_ALIGN;
     AttendParams p = attend_params(B, heads, kv_heads, D, H, W, L, scale);

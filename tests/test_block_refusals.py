@@ -63,8 +63,15 @@ def test_sizes_that_no_launch_counts(lib):
     assert lib.gspn_proxy_project_fused_bwd_bytes(1 << 18, 1024, 8, 1, 1, 1, 1) > 0
     assert lib.gspn_proxy_project_fused_bwd_bytes(1 << 22, 8, 8, 5, 8, 1, 1) > 0
     assert lib.gspn_proxy_project_fused(p, p, p, p, p, 1 << 24, 8, 8, 5, 8, 1, 1, None) == UNSUPPORTED
+    assert lib.gspn_proxy_project_fused(p, p, p, p, p, 1, 1 << 30, 1, 1, 1, 1, 1, None) == UNSUPPORTED
     tokens = (64, 64, 64, 8, 1, 1, 1 << 24)
     assert lib.gspn_cross_attention(p, p, p, p, p, p, p, 1 << 62, *tokens, 0.3, 1, None) == UNSUPPORTED
+
+
+def test_refusals_come_before_the_workspace(lib):
+    """A backward call without a workspace that is refused anyway says why."""
+    assert lib.gspn_gated_project_bwd(p, p, p, p, p, p, p, None, 0, 2, 16, 8, 5, 20000, 1, 1, None) == UNSUPPORTED
+    assert lib.gspn_cross_attention_bwd(*(p,) * 10, None, 0, 2, 4, 2, 12, 5, 7, 33, 0.25, 1, None) == UNSUPPORTED
 
 
 def test_attention_refuses_on_the_host(lib):
