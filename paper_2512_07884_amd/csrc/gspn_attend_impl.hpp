@@ -554,8 +554,8 @@ template <typename T> __global__ void __launch_bounds__(256) attend_join_kernel(
 // Two launches: gq (and delta) with a lane per position as in the forward call, then gk and gv with a lane per token and the positions
 // walked in stages.  p and ds are rounded to the storage type for the products, everything else is fp32.
 
-// gq, and delta for the launch after it; positions and tokens as in attend_kernel.  Up to 64 tokens delta is the sum over the tokens, in a pass of its own
-// over what LDS holds; else the product of gout and out, which the rounding of out puts off by e: since the weights of a position add up to 1, the sum
+// gq, and delta for the launch after it; positions and tokens as in attend_kernel.  Where up to 64 tokens take part delta is the sum over them, in a pass
+// of its own; else the product of gout and out, which the rounding of out puts off by e: since the weights of a position add up to 1, the sum
 // of its ds is then -e, and the second launch is given delta without it.
 template <typename T, int KS> struct AttendGradShape {
     static constexpr int TB = 64, ROW = along_pitch<T, KS>(), STAGE = TB * 2 * ROW, MAP = MapTile<T, KS>::BYTES;
@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_grad_waves(sizeo
     const unsigned item = xcd_contiguous_item(blockIdx.x, gridDim.x);
     const int group = item / p.workers, worker = item - group * p.workers, head = group % p.kv, b = group / p.kv;
     const float c2 = p.scale * LOG2E;
-    const bool few = p.L <= 64;
+    bool few = p.L <= 64;                                            // (of the tokens that take part: once they have been counted)
 
     constexpr bool AHEAD = attend_grad_ahead(sizeof(T) == 4, KS);
     Map maps[AHEAD ? 3 : 1];
@@ -675,6 +675,13 @@ __global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_grad_waves(sizeo
         if (AHEAD && tile < tiles) fetch(tile);
         all_tokens<T, KS, 64 * WAVES>(p, b, head, rows, lds, S::ROW, vt, S::ROW, words, tid);
         __syncthreads();
+        if (!few && p.mask) {
+            int have = 0;
+            for (int i = lane; i < rows / 32; i += 64) have += __popc(words[i]);
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) have += __shfl_xor(have, d);
+            few = __builtin_amdgcn_readfirstlane(have) <= 64;
+        }
         while (tile < tiles) {
             if (!AHEAD) fetch(tile);
             const size_t at = plane;
@@ -699,9 +706,39 @@ __global__ void __launch_bounds__(64 * WAVES, RESIDENT ? attend_grad_waves(sizeo
         char* const buf = lds + S::BUFFERS * S::STAGE + wave * S::MAP;
         const int stages = (p.L + S::TB - 1) / S::TB;
         fetch(min(worker * WAVES + wave, tiles - 1));                // (waves past the end: the last tile again, the same bits)
+        if (!few && p.mask) {
+            int have = 0;
+            for (int t = tid; t < p.L; t += 256) have += p.mask[(size_t)b * p.L + t] != 0;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) have += __shfl_xor(have, d);
+            int* const counts = (int*)lds;
+            if (lane == 0) counts[wave] = have;
+            __syncthreads();
+            few = __builtin_amdgcn_readfirstlane(counts[0] + counts[1] + counts[2] + counts[3]) <= 64;
+            __syncthreads();
+        }
+        start(buf);
+        if (few) {                                                   // over the tokens once more, with nothing on its way meanwhile
+#pragma unroll 1
+            for (int st = 0; st < stages; ++st) {
+                TokenStage<T, KS, S::TB> here;
+                here.fetch(p, b, head, st * S::TB, tid);
+                const uint64_t in = here.bits(0);
+                if (!in) continue;                                   // (the same for all waves)
+                lds_barrier();
+                here.put(lds, S::ROW, lds + S::TB * S::ROW, S::ROW, tid);
+                lds_barrier();
+#pragma unroll 1
+                for (int i = 0; i < S::TB / 32; ++i) {
+                    const uint32_t word = (uint32_t)(in >> (32 * i));
+                    if (word) sum_delta(lds + 32 * i * S::ROW, lds + (S::TB + 32 * i) * S::ROW, word);
+                }
+            }
+            delta = other_half_sum(delta);
+            lds_barrier();
+        }
         TokenStage<T, KS, S::TB> next;
         next.fetch(p, b, head, 0, tid);
-        start(buf);
         for (int st = 0; st < stages; ++st) {
             char* const kt = lds + (S::BUFFERS == 2 ? st & 1 : 0) * S::STAGE;
             char* const vt = kt + S::TB * S::ROW;

@@ -147,6 +147,31 @@ def test_what_masked_tokens_hold_is_never_used(dtype):
             assert all(torch.equal(a, b) for a, b in zip(res[0], other)), (dtype, L)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("L, D, shape", [(80, 8, (9, 11)), (77, 64, (8, 8)), (200, 72, (5, 13)), (900, 128, (6, 9))], ids=str)
+def test_gradient_of_q_where_few_tokens_take_part(L, D, shape, dtype):
+    """A batch padded to L of which an image has 1, 2, 3, 10 or 64 tokens: gq has its own rounding alone, not that of out as well (with one token it is zero but for fp32).
+
+    Bounds: the kernel's weights are off by at most 2^-16 (scores of up to 16 in powers of two, a hundred roundings of 2^-24 at the most), its products by less, and ds
+    is multiplied to 2^-15 of itself in 16 bits (two roundings of 2^-8 at the worst): 2^-13 of the magnitudes that gq adds, and a rounding of gq."""
+    heads, counts = 2, (1, 2, 3, 10, 64)
+    B = len(counts)
+    q, k, v, g, _ = _inputs(B, heads, heads, D, *shape, L, dtype, 40)
+    mask = torch.arange(L)[None] < torch.tensor(counts)[:, None]
+    scale = D ** -0.5
+    val, _ = R.attend(q, k, v, mask, g, heads, heads, scale, dtype)
+    got = _run(q, k, v, mask, g, heads, heads, scale, dtype)["gq"].double().cpu()
+    N = shape[0] * shape[1]
+    Q, Gm = q.reshape(B, heads, D, N), g.reshape(B, heads, D, N)
+    K, V = (t.reshape(B, L, heads, D).permute(0, 2, 1, 3) for t in (k, v))
+    p = torch.softmax(torch.where(mask[:, None, :, None], scale * (K @ Q), -math.inf), 2)
+    mag = V.abs() @ Gm.abs()
+    mag = p * (mag + (p * mag).sum(2, keepdim=True))
+    bound = 2.0 ** -13 * scale * (K.abs().transpose(2, 3) @ mag).reshape(q.shape) + R.half(dtype) * val["gq"].abs() + R.TINY[dtype]
+    worst = ((got - val["gq"]).abs() - bound).amax((1, 2, 3))
+    assert (worst <= 0).all(), (L, D, dtype, worst.tolist())
+
+
 def test_stretches_give_what_one_pass_gives():
     """The same call with and without the workspace it asks for."""
     import paper_2512_07884_amd as G
